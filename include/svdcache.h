@@ -23,6 +23,13 @@
  *   svdcache_basis_overlap / svdcache_rebase_state / svdcache_basis_similarity
  *                                                        basis reuse across prompts and refits (Sec. 3.3)
  *
+ * and, for the time steps on which a block's output is computed rather than forecast, the operators of a block whose
+ * linear layers run in 8 bits (the method is measured on such models too, Table 3):
+ *
+ *   svdcache_rms_norm8   the block's output enters the residual stream; its norm goes on in 8 bits (and / or plain)
+ *   svdcache_quantize8   a matrix of activations or weights in 8 bits
+ *   svdcache_matmul8     product of 8-bit activations and weights with bias, activation and an 8-bit result if wanted
+ *
  * General conventions
  *   - Every data pointer is a DEVICE pointer (HIP global memory) unless the
  *     argument is documented as "host".  The structs are host memory.
@@ -49,8 +56,9 @@
 extern "C" {
 #endif
 
-/* storage type of F, R and Fhat; arithmetic always accumulates in float32 or wider */
-typedef enum { SVDC_F32 = 0, SVDC_BF16 = 1 } svdc_dtype;
+/* storage type of F, R and Fhat; arithmetic always accumulates in float32 or wider.  SVDC_E4M3 is a type of results of
+ * svdcache_matmul8 alone. */
+typedef enum { SVDC_F32 = 0, SVDC_BF16 = 1, SVDC_E4M3 = 2 } svdc_dtype;
 
 /* Arithmetic of the bf16 matrix-core kernels (ignored by the float32 / general kernels).
  *   SVDC_PRECISE  V, C and S enter the products as bf16 high + low parts (about 16 significant
@@ -312,6 +320,96 @@ int32_t svdcache_rebase_state(const svdc_shape* shape, const float* M, const flo
 int32_t svdcache_basis_similarity(const svdc_shape* shape, const float* V_a, const float* sigma_a,
                                   const float* V_b, const float* sigma_b, float* sim_dir, float* sim_sigma,
                                   void* stream);
+
+/* ---- Operators of a block in 8 bits --------------------------------------------------------------------------------
+ *
+ * A matrix [rows, D] "in 8 bits" is a pair of dense buffers:
+ *   Q       rows x Dp bytes, Dp = D rounded up to 128: e4m3 values (4 bits of exponent, 3 of mantissa, no infinity; 0x7f / 0xff
+ *           are NaN), row-major; the columns D .. Dp-1 hold zeros.  16-byte aligned.
+ *   scales  one byte per row and 128 columns, the row stride Dp / 128 rounded up to 4 bytes (spare bytes hold 127): the scale is
+ *           2^(byte - 127).  4-byte aligned.  For weights one byte serves 128 rows too: ceil(rows / 128) rows of scales.
+ * and stands for Q * scale.  A block's scale is 2^e for the least e with amax <= 448 * 2^e, e in -126 .. 126, and 1 for a block of
+ * zeros; values are rounded to nearest, ties to even.  amax leaves NaN out and counts an infinity as the largest float32; NaN and
+ * infinities become NaN, so that they reach every result that depends on them.  Scales are powers of two because the matrix cores
+ * of gfx950 apply such scales inside the product.
+ *
+ * svdcache_q8_bytes / svdcache_q8_scale_bytes   sizes of the two buffers; block_rows 1 or 128.  0 for sizes out of range.  rows in
+ * 0 .. 2^31 - 1 and D in 1 .. 2^20 here and below; calls with rows = 0 return SVDC_OK and launch nothing. */
+size_t svdcache_q8_bytes(int64_t rows, int32_t D);
+size_t svdcache_q8_scale_bytes(int64_t rows, int32_t D, int32_t block_rows);
+
+/* One norm.  Strides are in elements, at least D, any alignment; rows * stride at most 2^48.  Those of tensors that are NULL are
+ * not read. */
+typedef struct {
+  int64_t rows;
+  int32_t D;
+  int32_t dtype;     /* svdc_dtype of X, H and Y: F32 or BF16 */
+  int32_t dtype_f;   /* svdc_dtype of F: F32 or BF16; need not be that of X (a float32 stream, bf16 block outputs) */
+  float eps;         /* >= 0, finite */
+  int64_t ldx, ldf, ldh, ldy;
+} svdc_norm8;
+
+/* Residual addition and root-mean-square norm:
+ *   h = X + F                                        in float32, not rounded before the norm
+ *   y = h * (1 / sqrt(mean_over_row(h^2) + eps)) * gain
+ *   X       in   [rows, D] dtype
+ *   F       in   [rows, D] dtype_f, or NULL: h = X
+ *   gain    in   [D] float32, or NULL: 1
+ *   H       out  [rows, D] dtype, h rounded; NULL if not wanted; may be the buffer X, or F if types and strides agree
+ *   Y       out  [rows, D] dtype, y rounded; NULL if not wanted
+ *   Q, scales  out  y in 8 bits (one scale per row and 128 columns); both NULL if not wanted
+ * At least one of Y and Q is given; outputs overlap neither each other nor inputs but as said.  Pointers are aligned to their elements,
+ * Q to 16 bytes, scales to 4.  A row of zeros gives zeros where eps > 0. */
+int32_t svdcache_rms_norm8(const svdc_norm8* p, const void* X, const void* F, const float* gain, void* H, void* Y, void* Q,
+                           void* scales, void* stream);
+
+/* One matrix to be held in 8 bits. */
+typedef struct {
+  int64_t rows;
+  int32_t D;
+  int32_t dtype;       /* svdc_dtype of X: F32 or BF16 */
+  int64_t ldx;         /* as in svdc_norm8 */
+  int32_t block_rows;  /* rows that share a scale: 1 (activations) or 128 (weights) */
+  int32_t reserved;    /* set to 0 */
+} svdc_quant8;
+
+/* (Q, scales) <- X [rows, D] dtype. */
+int32_t svdcache_quantize8(const svdc_quant8* p, const void* X, void* Q, void* scales, void* stream);
+
+/* What is applied to a product's sums: nothing; x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))); or a gate, silu(gate row) * (row
+ * it gates) with silu(x) = x / (1 + exp(-x)). */
+typedef enum { SVDC_ACT_NONE = 0, SVDC_ACT_GELU = 1, SVDC_ACT_SWIGLU = 2 } svdc_act;
+
+/* One product. */
+typedef struct {
+  int64_t M;        /* rows of A and of Out */
+  int32_t N, K;     /* columns of Out (1 .. 2^24), columns of A and W (1 .. 2^20) */
+  int32_t dtype;    /* svdc_dtype of Out: F32, BF16 or E4M3 (8 bits, with scales per row and 128 columns) */
+  int32_t act;      /* svdc_act */
+  int64_t ldo;      /* row stride of Out in elements, at least N, M * ldo at most 2^48; not read for E4M3 */
+} svdc_matmul8;
+
+/* Bytes of device workspace that svdcache_matmul8 needs for this product: 0 for most (and for an invalid one); products of few
+ * rows over a long K keep partial sums there. */
+size_t svdcache_matmul8_workspace_bytes(const svdc_matmul8* p);
+
+/* Product of matrices in 8 bits:
+ *   z[m][n]   = sum_k A[m][k] W[n][k] + bias[n]
+ *   Out[m][n] = act(z)[m][n]
+ * For results in float32 the sums are float32 sums.  For results in bfloat16 and in 8 bits they are those of the 8-bit matrix instructions: 8 products at a
+ * time with 13 bits below the largest, these in float32 (about 4e-5 of a result, against 1.7e-3 and more by its rounding), at twice the rate.
+ *   A, A_scales   in   [M, K] in 8 bits, one scale per row and 128 columns
+ *   W, W_scales   in   [Nw, K] in 8 bits, one scale per 128 rows and 128 columns; Nw = N, and 2 N for SVDC_ACT_SWIGLU: rows
+ *                      0 .. N-1 are gates, rows N .. 2N-1 what they multiply
+ *   bias          in   [Nw] float32, 4-byte aligned, or NULL: 0
+ *   Out           out  [M, N] dtype with row stride ldo, aligned to its elements; for E4M3 Q of [M, N] in 8 bits
+ *   Out_scales    out  its scales for E4M3, else not read
+ *   workspace     device scratch of svdcache_matmul8_workspace_bytes() bytes, 256-byte aligned, NULL where that is 0.  It belongs to the call until it
+ *                 has completed on the stream: calls in flight on different streams need one each.
+ * Results do not depend on anything but the arguments (no atomics). */
+int32_t svdcache_matmul8(const svdc_matmul8* p, const void* A, const void* A_scales, const void* W, const void* W_scales,
+                         const float* bias, void* Out, void* Out_scales, void* workspace, size_t workspace_bytes,
+                         void* stream);
 
 #ifdef __cplusplus
 }

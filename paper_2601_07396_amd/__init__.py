@@ -18,6 +18,10 @@ from .binding import (
     svdcache_select_rank, svdcache_truncate_basis, svdcache_extrapolation_weights, svdcache_forecast_combine,
     svdcache_basis_overlap, svdcache_rebase_state, svdcache_basis_similarity,
     make_shape, fit_basis, fit_basis_for_energy, pack_basis, save_basis, load_basis,
+    Norm8, Quant8, Matmul8, SVDC_E4M3, SVDC_ACT_NONE, SVDC_ACT_GELU, SVDC_ACT_SWIGLU, svdcache_q8_bytes,
+    svdcache_q8_scale_bytes, svdcache_rms_norm8, svdcache_quantize8, svdcache_matmul8_workspace_bytes,
+    svdcache_matmul8, make_norm8, make_quant8, make_matmul8, alloc_q8, alloc_matmul8_workspace, rms_norm8, quantize8,
+    matmul8,
 )
 
 __all__ = [
@@ -30,4 +34,8 @@ __all__ = [
     "svdcache_full_step_packed", "svdcache_forecast_packed", "alloc_packed_state", "svdcache_select_rank", "svdcache_truncate_basis", "svdcache_extrapolation_weights",
     "svdcache_forecast_combine", "svdcache_basis_overlap", "svdcache_rebase_state", "svdcache_basis_similarity",
     "make_shape", "fit_basis", "fit_basis_for_energy", "pack_basis", "save_basis", "load_basis",
+    "Norm8", "Quant8", "Matmul8", "SVDC_E4M3", "SVDC_ACT_NONE", "SVDC_ACT_GELU", "SVDC_ACT_SWIGLU",
+    "svdcache_q8_bytes", "svdcache_q8_scale_bytes", "svdcache_rms_norm8", "svdcache_quantize8",
+    "svdcache_matmul8_workspace_bytes", "svdcache_matmul8", "make_norm8", "make_quant8", "make_matmul8", "alloc_q8",
+    "alloc_matmul8_workspace", "rms_norm8", "quantize8", "matmul8",
 ]

@@ -34,6 +34,23 @@ class FitParams(C.Structure):
                 ("jacobi_max_sweeps", C.c_int32), ("reserved", C.c_int32)]
 
 
+class Norm8(C.Structure):
+    """Mirror of svdc_norm8."""
+    _fields_ = [("rows", C.c_int64), ("D", C.c_int32), ("dtype", C.c_int32), ("dtype_f", C.c_int32), ("eps", C.c_float),
+                ("ldx", C.c_int64), ("ldf", C.c_int64), ("ldh", C.c_int64), ("ldy", C.c_int64)]
+
+
+class Quant8(C.Structure):
+    """Mirror of svdc_quant8."""
+    _fields_ = [("rows", C.c_int64), ("D", C.c_int32), ("dtype", C.c_int32), ("ldx", C.c_int64), ("block_rows", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class Matmul8(C.Structure):
+    """Mirror of svdc_matmul8."""
+    _fields_ = [("M", C.c_int64), ("N", C.c_int32), ("K", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32), ("ldo", C.c_int64)]
+
+
 EXPORTS = {
     "svdcache_version": (C.c_int32, []),
     "svdcache_strerror": (C.c_char_p, [C.c_int32]),
@@ -72,6 +89,12 @@ EXPORTS = {
     "svdcache_forecast_combine": (C.c_int32, [C.POINTER(Shape), C.c_int32, C.POINTER(C.c_void_p),
                                               C.POINTER(C.c_float), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                               C.c_void_p, C.c_void_p]),
+    "svdcache_q8_bytes": (C.c_size_t, [C.c_int64, C.c_int32]),
+    "svdcache_q8_scale_bytes": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int32]),
+    "svdcache_rms_norm8": (C.c_int32, [C.POINTER(Norm8)] + [C.c_void_p] * 8),
+    "svdcache_quantize8": (C.c_int32, [C.POINTER(Quant8)] + [C.c_void_p] * 4),
+    "svdcache_matmul8_workspace_bytes": (C.c_size_t, [C.POINTER(Matmul8)]),
+    "svdcache_matmul8": (C.c_int32, [C.POINTER(Matmul8)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]),
 }
 
 _lib = None
@@ -116,7 +139,7 @@ def _load_fast_calls(lib):
         spec = importlib.util.spec_from_file_location("_fast_calls", path)
         fast = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(fast)
-        fast.bind({name: C.cast(getattr(lib, name), C.c_void_p).value for name in EXPORTS}, Shape)
+        fast.bind({name: C.cast(getattr(lib, name), C.c_void_p).value for name in EXPORTS}, Shape, Norm8, Quant8, Matmul8)
     except Exception as e:
         warnings.warn(f"{path} does not load ({e}): step calls take about 4 us more host time each; "
                       "build it again with `python -m paper_2601_07396_amd.build`", RuntimeWarning, stacklevel=3)
@@ -429,6 +452,148 @@ def svdcache_basis_similarity(shape: Shape, V_a, sigma_a, V_b, sigma_b, sim_dir,
     _check(rc, "svdcache_basis_similarity")
 
 
+# ---- operators of a block in 8 bits -------------------------------------------------------------
+
+SVDC_E4M3 = 2
+SVDC_ACT_NONE, SVDC_ACT_GELU, SVDC_ACT_SWIGLU = 0, 1, 2
+_ACTS = {"none": SVDC_ACT_NONE, "gelu": SVDC_ACT_GELU, "swiglu": SVDC_ACT_SWIGLU}
+_TORCH_OF_8 = {SVDC_F32: torch.float32, SVDC_BF16: torch.bfloat16, SVDC_E4M3: torch.float8_e4m3fn}
+_DTYPES_8 = {v: k for k, v in _TORCH_OF_8.items()}
+
+
+def _row_stride(name: str, t: torch.Tensor):
+    """(rows, D, row stride) of a tensor [..., D] whose rows lie at one stride."""
+    if t.dim() < 1 or t.shape[-1] < 1 or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: need [..., D] with a contiguous last dimension, got {tuple(t.shape)} with strides {t.stride()}")
+    D, rows, ld = t.shape[-1], t.numel() // t.shape[-1], None
+    step = None                                        # what the next dimension outwards has to have as its stride
+    for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if step is None:
+            ld, step = st, st * n
+        elif st != step:
+            raise ValueError(f"{name}: rows of {tuple(t.shape)} with strides {t.stride()} do not lie at one stride")
+        else:
+            step *= n
+    return rows, D, D if ld is None or rows == 0 else ld
+
+
+def make_norm8(X: torch.Tensor, F: Optional[torch.Tensor] = None, H: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
+               eps: float = 1e-6) -> Norm8:
+    """Descriptor of a norm of X [..., D] (float32 or bfloat16) for tensors laid out like these; F may be of the other type."""
+    rows, D, ldx = _row_stride("X", X)
+    if X.dtype not in _DTYPES or (F is not None and F.dtype not in _DTYPES):
+        raise ValueError("X and F must be float32 or bfloat16")
+    p = Norm8(rows, D, _DTYPES[X.dtype], _DTYPES[(X if F is None else F).dtype], eps, ldx, D, D, D)
+    for name, field, t in (("F", "ldf", F), ("H", "ldh", H), ("Y", "ldy", Y)):
+        if t is not None:
+            r, d, ld = _row_stride(name, t)
+            if (r, d) != (rows, D):
+                raise ValueError(f"{name}: {tuple(t.shape)} is not {rows} rows of {D} columns")
+            setattr(p, field, ld)
+    return p
+
+
+def make_quant8(X: torch.Tensor, block_rows: int = 1) -> Quant8:
+    """Descriptor of the quantisation of X [..., D] with a scale per block_rows (1 or 128) rows and 128 columns."""
+    rows, D, ldx = _row_stride("X", X)
+    if X.dtype not in _DTYPES:
+        raise ValueError("X must be float32 or bfloat16")
+    return Quant8(rows, D, _DTYPES[X.dtype], ldx, block_rows, 0)
+
+
+def make_matmul8(M: int, N: int, K: int, dtype: torch.dtype = torch.bfloat16, act: str = "none", ldo: int = 0) -> Matmul8:
+    """Descriptor of Out [M, N] = act(A [M, K] W^T + bias) with Out of `dtype` (float32, bfloat16 or float8_e4m3fn) and row stride
+    ldo (0: N).  act: "none", "gelu" or "swiglu" (W then holds 2 N rows)."""
+    if dtype not in _DTYPES_8 or act not in _ACTS:
+        raise ValueError("dtype is one of float32, bfloat16 and float8_e4m3fn, act one of " + ", ".join(_ACTS))
+    return Matmul8(M, N, K, _DTYPES_8[dtype], _ACTS[act], ldo or N)
+
+
+def svdcache_q8_bytes(rows: int, D: int) -> int:
+    return load_library().svdcache_q8_bytes(rows, D)
+
+
+def svdcache_q8_scale_bytes(rows: int, D: int, block_rows: int = 1) -> int:
+    return load_library().svdcache_q8_scale_bytes(rows, D, block_rows)
+
+
+def svdcache_matmul8_workspace_bytes(p: Matmul8) -> int:
+    return load_library().svdcache_matmul8_workspace_bytes(C.byref(p))
+
+
+_BYTES = (torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.uint8)
+
+
+def _bytes_of(name: str, t, need: int):
+    """Q and scales are dense tensors of one byte an element, of exactly the size that the sizes imply."""
+    if t.dtype not in _BYTES or not t.is_contiguous() or t.numel() != need:
+        raise ValueError(f"{name}: need a contiguous tensor of {need} bytes, got {t.dtype} {tuple(t.shape)} contiguous={t.is_contiguous()}")
+
+
+def _check_q8(name: str, Q, scales, rows: int, D: int, block_rows: int = 1):
+    _bytes_of(name, Q, svdcache_q8_bytes(rows, D))
+    _bytes_of(name + " scales", scales, svdcache_q8_scale_bytes(rows, D, block_rows))
+
+
+def _rows_like(name: str, t, rows: int, D: int, ld: int, dtype: int):
+    """The C ABI describes each tensor by (rows, D, row stride, dtype): refuse one that is laid out otherwise."""
+    if t.dtype != _TORCH_OF[dtype]:
+        raise ValueError(f"{name}: dtype {t.dtype} is not {_TORCH_OF[dtype]}")
+    r, d, have = _row_stride(name, t)
+    if (r, d) != (rows, D) or (r > 1 and have != ld):
+        raise ValueError(f"{name}: {tuple(t.shape)} with row stride {have} is not {rows} rows of {D} columns with row stride {ld}")
+
+
+def svdcache_rms_norm8(p: Norm8, X, F, gain, H, Y, Q, scales):
+    """H = X + F and its norm: Y plain, (Q, scales) in 8 bits.  F, gain, H, Y and (Q, scales) may be None."""
+    if _fast_call("rms_norm8", p, X, F, gain, H, Y, Q, scales):
+        return
+    for name, t, ld, dtype in (("X", X, p.ldx, p.dtype), ("F", F, p.ldf, p.dtype_f), ("H", H, p.ldh, p.dtype), ("Y", Y, p.ldy, p.dtype)):
+        if t is not None:
+            _rows_like(name, t, p.rows, p.D, ld, dtype)
+    _dense_f32(p.D, "[D]", gain=gain)
+    if (Q is None) != (scales is None):
+        raise ValueError("Q and scales go together")
+    if Q is not None:
+        _check_q8("Q", Q, scales, p.rows, p.D)
+    _need_gpu(X, F, gain, H, Y, Q, scales)
+    rc = load_library().svdcache_rms_norm8(C.byref(p), _ptr(X), _ptr(F), _ptr(gain), _ptr(H), _ptr(Y), _ptr(Q), _ptr(scales), _stream())
+    _check(rc, "svdcache_rms_norm8")
+
+
+def svdcache_quantize8(p: Quant8, X, Q, scales):
+    if _fast_call("quantize8", p, X, Q, scales):
+        return
+    _rows_like("X", X, p.rows, p.D, p.ldx, p.dtype)
+    _check_q8("Q", Q, scales, p.rows, p.D, p.block_rows)
+    _need_gpu(X, Q, scales)
+    rc = load_library().svdcache_quantize8(C.byref(p), _ptr(X), _ptr(Q), _ptr(scales), _stream())
+    _check(rc, "svdcache_quantize8")
+
+
+def svdcache_matmul8(p: Matmul8, A, A_scales, W, W_scales, bias, Out, Out_scales=None, workspace=None):
+    """Out = act(A W^T + bias).  workspace: alloc_matmul8_workspace(p), one for each call in flight on a stream of its own."""
+    if _fast_call("matmul8", p, A, A_scales, W, W_scales, bias, Out, Out_scales, workspace):
+        return
+    wide = 2 * p.N if p.act == SVDC_ACT_SWIGLU else p.N
+    _check_q8("A", A, A_scales, p.M, p.K)
+    _bytes_of("W", W, wide * ((p.K + 127) // 128 * 128))
+    _bytes_of("W scales", W_scales, svdcache_q8_scale_bytes(wide, p.K, 128))
+    _dense_f32(wide, "[rows of W]", bias=bias)
+    if p.dtype == SVDC_E4M3:
+        if Out_scales is None:
+            raise ValueError("Out_scales: a result in 8 bits has scales")
+        _check_q8("Out", Out, Out_scales, p.M, p.N)
+    else:
+        _rows_like("Out", Out, p.M, p.N, p.ldo, p.dtype)
+    _need_gpu(A, A_scales, W, W_scales, bias, Out, Out_scales, workspace)
+    rc = load_library().svdcache_matmul8(C.byref(p), _ptr(A), _ptr(A_scales), _ptr(W), _ptr(W_scales), _ptr(bias), _ptr(Out), _ptr(Out_scales),
+                                         _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    _check(rc, "svdcache_matmul8")
+
+
 # ---- conveniences that only allocate (torch owns the memory) ------------------------------------
 
 def fit_basis(F: torch.Tensor, k: int, p: int = 0, q: int = 0, seed: int = 0, max_sweeps: int = 0,
@@ -515,3 +680,50 @@ def pack_basis(shape: Shape, V: torch.Tensor):
     packed = torch.empty(n, device=V.device, dtype=torch.uint8)
     svdcache_pack_basis(shape, V, packed)
     return packed
+
+
+def alloc_q8(rows: int, D: int, device, block_rows: int = 1):
+    """(Q, scales) for a matrix [rows, D] in 8 bits: float8_e4m3fn [rows, D rounded up to 128], float8_e8m0fnu [rows / block_rows, ...]."""
+    nq, ns = svdcache_q8_bytes(rows, D), svdcache_q8_scale_bytes(rows, D, block_rows)
+    if rows < 0 or (rows and not (nq and ns)):
+        raise SvdcError(-2, "svdcache_q8_bytes")
+    tall = (rows + block_rows - 1) // block_rows
+    Q = torch.empty(nq, device=device, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    scales = torch.empty(ns, device=device, dtype=torch.uint8).view(torch.float8_e8m0fnu)
+    wide = (D + 127) // 128
+    return Q.view(rows, wide * 128), scales.view(tall, (wide + 3) // 4 * 4)
+
+
+def alloc_matmul8_workspace(p: Matmul8, device):
+    """Workspace of svdcache_matmul8 for this product, or None where it needs none."""
+    n = svdcache_matmul8_workspace_bytes(p)
+    return torch.empty(n, device=device, dtype=torch.uint8) if n else None
+
+
+def rms_norm8(X: torch.Tensor, F: Optional[torch.Tensor] = None, gain: Optional[torch.Tensor] = None, eps: float = 1e-6):
+    """(H, Q, scales): H = X + F and its norm in 8 bits, in new tensors."""
+    H = torch.empty(X.shape, device=X.device, dtype=X.dtype)
+    p = make_norm8(X, F, H, None, eps)
+    Q, scales = alloc_q8(p.rows, p.D, X.device)
+    svdcache_rms_norm8(p, X, F, gain, H, None, Q, scales)
+    return H, Q, scales
+
+
+def quantize8(X: torch.Tensor, block_rows: int = 1):
+    """(Q, scales) of X [..., D] in new tensors; block_rows 1 for activations, 128 for weights."""
+    p = make_quant8(X, block_rows)
+    Q, scales = alloc_q8(p.rows, p.D, X.device, block_rows)
+    svdcache_quantize8(p, X, Q, scales)
+    return Q, scales
+
+
+def matmul8(A, A_scales, W, W_scales, K: int, bias: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16, act: str = "none"):
+    """act(A W^T + bias) in a new tensor [rows of A, N]; (Out, Out_scales) for dtype float8_e4m3fn.  A and W as alloc_q8 shapes them."""
+    N = W.shape[0] // 2 if act == "swiglu" else W.shape[0]
+    p = make_matmul8(A.shape[0], N, K, dtype, act)
+    if dtype == torch.float8_e4m3fn:
+        Out, Out_scales = alloc_q8(p.M, p.N, A.device)
+    else:
+        Out, Out_scales = torch.empty(p.M, p.N, device=A.device, dtype=dtype), None
+    svdcache_matmul8(p, A, A_scales, W, W_scales, bias, Out, Out_scales, alloc_matmul8_workspace(p, A.device))
+    return Out if Out_scales is None else (Out, Out_scales)

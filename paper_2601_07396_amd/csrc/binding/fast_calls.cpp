@@ -15,7 +15,8 @@
 
 namespace {
 
-PyTypeObject* shape_type;       // binding.Shape
+// binding.Shape, Norm8, Quant8 and Matmul8
+PyTypeObject *shape_type, *norm8_type, *quant8_type, *matmul8_type;
 
 // addresses inside the library that the binding loaded
 struct Library {
@@ -27,19 +28,23 @@ struct Library {
   decltype(&svdcache_forecast) forecast;
   decltype(&svdcache_forecast_packed) forecast_packed;
   decltype(&svdcache_forecast_combine) forecast_combine;
+  decltype(&svdcache_rms_norm8) rms_norm8;
+  decltype(&svdcache_quantize8) quantize8;
+  decltype(&svdcache_matmul8) matmul8;
 } lib;
 
 // The arguments of one call; `ok` falls when one of them is not ordinary.
-struct Args {
-  svdc_shape s;
+template <typename Problem>
+struct Arguments {
+  Problem s;
   bool ok = false;
 
-  explicit Args(PyObject* shape) {
+  Arguments(PyObject* problem, PyTypeObject* type) {
     Py_buffer view;
-    if (Py_TYPE(shape) != shape_type || PyObject_GetBuffer(shape, &view, PyBUF_SIMPLE) != 0) return;
+    if (Py_TYPE(problem) != type || PyObject_GetBuffer(problem, &view, PyBUF_SIMPLE) != 0) return;
     if (view.len == (Py_ssize_t)sizeof(s)) {
       std::memcpy(&s, view.buf, sizeof(s));
-      ok = s.dtype == SVDC_F32 || s.dtype == SVDC_BF16;
+      ok = true;
     }
     PyBuffer_Release(&view);
   }
@@ -51,21 +56,12 @@ struct Args {
     ok = false;
     return nullptr;
   }
-  void* features(PyObject* o) {             // [B, N, D] with the strides of the shape
-    const at::Tensor* t = tensor(o);
-    if (!t) return nullptr;
-    ok = t->scalar_type() == (s.dtype == SVDC_F32 ? at::kFloat : at::kBFloat16) && t->dim() == 3 && t->size(0) == s.B &&
-         t->size(1) == s.N && t->size(2) == s.D && t->stride(0) == s.block_stride && t->stride(1) == s.ldf && t->stride(2) == 1;
-    return ok ? t->data_ptr() : nullptr;
-  }
   void* dense(PyObject* o, int64_t count) { // contiguous float32
     const at::Tensor* t = tensor(o);
     if (!t) return nullptr;
     ok = t->scalar_type() == at::kFloat && t->is_contiguous() && t->numel() == count;
     return ok ? t->data_ptr() : nullptr;
   }
-  void* basis(PyObject* o) { return dense(o, (int64_t)s.B * s.D * s.k); }
-  void* state(PyObject* o) { return dense(o, (int64_t)s.B * s.N * s.k); }
   void* bytes(PyObject* o, size_t need, size_t* have = nullptr) {
     const at::Tensor* t = tensor(o);
     if (!t) return nullptr;
@@ -74,6 +70,19 @@ struct Args {
     if (have) *have = n;
     return ok ? t->data_ptr() : nullptr;
   }
+};
+
+struct Args : Arguments<svdc_shape> {
+  explicit Args(PyObject* shape) : Arguments(shape, shape_type) { ok = ok && (s.dtype == SVDC_F32 || s.dtype == SVDC_BF16); }
+  void* features(PyObject* o) {             // [B, N, D] with the strides of the shape
+    const at::Tensor* t = tensor(o);
+    if (!t) return nullptr;
+    ok = t->scalar_type() == (s.dtype == SVDC_F32 ? at::kFloat : at::kBFloat16) && t->dim() == 3 && t->size(0) == s.B &&
+         t->size(1) == s.N && t->size(2) == s.D && t->stride(0) == s.block_stride && t->stride(1) == s.ldf && t->stride(2) == 1;
+    return ok ? t->data_ptr() : nullptr;
+  }
+  void* basis(PyObject* o) { return dense(o, (int64_t)s.B * s.D * s.k); }
+  void* state(PyObject* o) { return dense(o, (int64_t)s.B * s.N * s.k); }
   void* packed_basis(PyObject* o) { return ok ? bytes(o, lib.packed_basis_bytes(&s)) : nullptr; }
   void* optional(PyObject* o, void* (Args::*get)(PyObject*)) { return o == Py_None ? nullptr : (this->*get)(o); }
   // Python's own numbers only: the conversion of any other object runs its code, which may change the list that is being read
@@ -89,14 +98,44 @@ struct Args {
   }
 };
 
+// Matrices of the operators in 8 bits.
+template <typename Problem>
+struct Args8 : Arguments<Problem> {
+  using Arguments<Problem>::Arguments;
+  using Arguments<Problem>::ok;
+  using Arguments<Problem>::tensor;
+
+  void* rows(PyObject* o, int64_t n, int64_t D, int64_t ld, int32_t dtype) {   // [n, D] with row stride ld, or contiguous [..., D]
+    const at::Tensor* t = tensor(o);
+    if (!t) return nullptr;
+    const int64_t d = t->dim();
+    ok = (dtype == SVDC_F32 || dtype == SVDC_BF16) && t->scalar_type() == (dtype == SVDC_F32 ? at::kFloat : at::kBFloat16) && d >= 2 &&
+         t->size(d - 1) == D && t->numel() == n * D &&
+         (d == 2 && t->stride(1) == 1 ? n <= 1 || t->stride(0) == ld : ld == D && t->is_contiguous());
+    return ok ? t->data_ptr() : nullptr;
+  }
+  void* eight(PyObject* o, int64_t count) {                                    // dense, a byte an element
+    const at::Tensor* t = tensor(o);
+    if (!t) return nullptr;
+    const auto type = t->scalar_type();
+    ok = (type == at::kFloat8_e4m3fn || type == at::kFloat8_e8m0fnu || type == at::kByte) && t->is_contiguous() && t->numel() == count;
+    return ok ? t->data_ptr() : nullptr;
+  }
+  void* values(PyObject* o, int64_t n, int64_t D) { return eight(o, n * blocks(D) * 128); }
+  void* scales(PyObject* o, int64_t n, int64_t D, int64_t block_rows) {
+    return eight(o, (n + block_rows - 1) / block_rows * ((blocks(D) + 3) / 4 * 4));
+  }
+  static int64_t blocks(int64_t D) { return (D + 127) / 128; }
+};
+
 // Runs `body(args)`, which returns a call to make without the interpreter lock; None where the arguments are not ordinary.
-template <typename Body>
-PyObject* call(PyObject* const* argv, Py_ssize_t argc, Py_ssize_t want, Body body) {
+template <typename A, typename... Type, typename Body>
+PyObject* call_with(PyObject* const* argv, Py_ssize_t argc, Py_ssize_t want, Body body, Type*... type) {
   int32_t rc = 0;
   bool made = false;
   if (argc == want && lib.full_step) {
     try {
-      Args a(argv[0]);
+      A a(argv[0], type...);
       auto launch = body(a);
       if (a.ok) {
         void* stream = c10::hip::getCurrentHIPStream().stream();
@@ -111,6 +150,11 @@ PyObject* call(PyObject* const* argv, Py_ssize_t argc, Py_ssize_t want, Body bod
   if (made) return PyLong_FromLong(rc);
   PyErr_Clear();
   Py_RETURN_NONE;
+}
+
+template <typename Body>
+PyObject* call(PyObject* const* argv, Py_ssize_t argc, Py_ssize_t want, Body body) {
+  return call_with<Args>(argv, argc, want, body);
 }
 
 PyObject* full_step(PyObject*, PyObject* const* v, Py_ssize_t n) {          // shape F V packed R S C alpha init
@@ -176,10 +220,51 @@ PyObject* forecast_combine(PyObject*, PyObject* const* v, Py_ssize_t n) {   // s
   });
 }
 
-// bind(addresses of the loaded library's functions by name, the class of the shape)
+PyObject* rms_norm8(PyObject*, PyObject* const* v, Py_ssize_t n) {          // norm8 X F gain H Y Q scales
+  return call_with<Args8<svdc_norm8>>(v, n, 8, [&](Args8<svdc_norm8>& a) {
+    const svdc_norm8& p = a.s;
+    void* X = a.rows(v[1], p.rows, p.D, p.ldx, p.dtype);
+    void* F = v[2] == Py_None ? nullptr : a.rows(v[2], p.rows, p.D, p.ldf, p.dtype_f);
+    void* gain = v[3] == Py_None ? nullptr : a.dense(v[3], p.D);
+    void* H = v[4] == Py_None ? nullptr : a.rows(v[4], p.rows, p.D, p.ldh, p.dtype);
+    void* Y = v[5] == Py_None ? nullptr : a.rows(v[5], p.rows, p.D, p.ldy, p.dtype);
+    void* Q = v[6] == Py_None ? nullptr : a.values(v[6], p.rows, p.D);
+    void* scales = v[7] == Py_None ? nullptr : a.scales(v[7], p.rows, p.D, 1);
+    a.ok = a.ok && (v[6] == Py_None) == (v[7] == Py_None);
+    return [=, &a](void* st) { return lib.rms_norm8(&a.s, X, F, (float*)gain, H, Y, Q, scales, st); };
+  }, norm8_type);
+}
+PyObject* quantize8(PyObject*, PyObject* const* v, Py_ssize_t n) {          // quant8 X Q scales
+  return call_with<Args8<svdc_quant8>>(v, n, 4, [&](Args8<svdc_quant8>& a) {
+    const svdc_quant8& p = a.s;
+    a.ok = a.ok && (p.block_rows == 1 || p.block_rows == 128);
+    void *X = a.rows(v[1], p.rows, p.D, p.ldx, p.dtype), *Q = a.values(v[2], p.rows, p.D),
+         *scales = a.ok ? a.scales(v[3], p.rows, p.D, p.block_rows) : nullptr;
+    return [=, &a](void* st) { return lib.quantize8(&a.s, X, Q, scales, st); };
+  }, quant8_type);
+}
+PyObject* matmul8(PyObject*, PyObject* const* v, Py_ssize_t n) {            // matmul8 A A_scales W W_scales bias Out Out_scales workspace
+  return call_with<Args8<svdc_matmul8>>(v, n, 9, [&](Args8<svdc_matmul8>& a) {
+    const svdc_matmul8& p = a.s;
+    const int64_t wide = p.act == SVDC_ACT_SWIGLU ? 2 * (int64_t)p.N : p.N;
+    const bool eight = p.dtype == SVDC_E4M3;
+    void *A = a.values(v[1], p.M, p.K), *As = a.scales(v[2], p.M, p.K, 1), *W = a.values(v[3], wide, p.K), *Ws = a.scales(v[4], wide, p.K, 128);
+    void* bias = v[5] == Py_None ? nullptr : a.dense(v[5], wide);
+    void* Out = eight ? a.values(v[6], p.M, p.N) : a.rows(v[6], p.M, p.N, p.ldo, p.dtype);
+    a.ok = a.ok && eight == (v[7] != Py_None);
+    void* Os = v[7] == Py_None ? nullptr : a.scales(v[7], p.M, p.N, 1);
+    size_t have = 0;
+    void* workspace = v[8] == Py_None ? nullptr : a.bytes(v[8], 1, &have);
+    return [=, &a](void* st) { return lib.matmul8(&a.s, A, As, W, Ws, (float*)bias, Out, Os, workspace, have, st); };
+  }, matmul8_type);
+}
+
+// bind(addresses of the loaded library's functions by name, the classes of the shape, the norm, the quantisation and the product)
 PyObject* bind(PyObject*, PyObject* args) {
-  PyObject *addresses, *type;
-  if (!PyArg_ParseTuple(args, "O!O!", &PyDict_Type, &addresses, &PyType_Type, &type)) return nullptr;
+  PyObject *addresses, *type[4];
+  if (!PyArg_ParseTuple(args, "O!O!O!O!O!", &PyDict_Type, &addresses, &PyType_Type, &type[0], &PyType_Type, &type[1], &PyType_Type, &type[2],
+                        &PyType_Type, &type[3]))
+    return nullptr;
   auto get = [&](const char* name) -> void* {
     PyObject* o = PyDict_GetItemString(addresses, name);
     return o ? PyLong_AsVoidPtr(o) : nullptr;
@@ -194,17 +279,23 @@ PyObject* bind(PyObject*, PyObject* args) {
   SVDC_BIND(forecast);
   SVDC_BIND(forecast_packed);
   SVDC_BIND(forecast_combine);
+  SVDC_BIND(rms_norm8);
+  SVDC_BIND(quantize8);
+  SVDC_BIND(matmul8);
 #undef SVDC_BIND
   if (PyErr_Occurred()) return nullptr;
   if (!l.packed_basis_bytes || !l.packed_state_bytes || !l.full_step || !l.full_step_residual_ema || !l.full_step_packed ||
-      !l.forecast || !l.forecast_packed || !l.forecast_combine) {
+      !l.forecast || !l.forecast_packed || !l.forecast_combine || !l.rms_norm8 || !l.quantize8 || !l.matmul8) {
     PyErr_SetString(PyExc_ValueError, "bind: an address is missing");
     return nullptr;
   }
   lib = l;
-  Py_INCREF(type);
-  Py_XDECREF(shape_type);
-  shape_type = reinterpret_cast<PyTypeObject*>(type);
+  PyTypeObject** const held[4] = {&shape_type, &norm8_type, &quant8_type, &matmul8_type};
+  for (int i = 0; i < 4; ++i) {
+    Py_INCREF(type[i]);
+    Py_XDECREF(*held[i]);
+    *held[i] = reinterpret_cast<PyTypeObject*>(type[i]);
+  }
   Py_RETURN_NONE;
 }
 
@@ -214,6 +305,9 @@ PyMethodDef methods[] = {{"full_step", (PyCFunction)(void (*)())full_step, METH_
                          {"forecast", (PyCFunction)(void (*)())forecast, METH_FASTCALL, nullptr},
                          {"forecast_packed", (PyCFunction)(void (*)())forecast_packed, METH_FASTCALL, nullptr},
                          {"forecast_combine", (PyCFunction)(void (*)())forecast_combine, METH_FASTCALL, nullptr},
+                         {"rms_norm8", (PyCFunction)(void (*)())rms_norm8, METH_FASTCALL, nullptr},
+                         {"quantize8", (PyCFunction)(void (*)())quantize8, METH_FASTCALL, nullptr},
+                         {"matmul8", (PyCFunction)(void (*)())matmul8, METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast_calls", "Step calls with ordinary arguments.", -1, methods,

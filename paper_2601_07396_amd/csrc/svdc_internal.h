@@ -52,6 +52,13 @@ int32_t launch_rebase_state(const svdc_shape& s, const float* M, const float* S_
 int32_t launch_basis_similarity(const svdc_shape& s, const float* V_a, const float* sigma_a, const float* V_b,
                                 const float* sigma_b, float* sim_dir, float* sim_sigma, hipStream_t st);
 
+// ---- operators of a block in 8 bits: rows8_kernels.hip, matmul8_kernels.hip ---------------------
+int32_t launch_rms_norm8(const svdc_norm8& p, const void* X, const void* F, const float* gain, void* H, void* Y, void* Q, void* scales, hipStream_t st);
+int32_t launch_quantize8(const svdc_quant8& p, const void* X, void* Q, void* scales, hipStream_t st);
+size_t matmul8_workspace_bytes(const svdc_matmul8& p);
+int32_t launch_matmul8(const svdc_matmul8& p, const void* A, const void* As, const void* W, const void* Ws, const float* bias, void* Out, void* Os,
+                       void* workspace, hipStream_t st);
+
 // ---- matrix-core kernels: mfma_kernels.hip -----------------------------------
 bool mfma_shape_supported(const svdc_shape& s);
 size_t mfma_packed_bytes(const svdc_shape& s);

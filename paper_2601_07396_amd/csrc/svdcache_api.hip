@@ -3,6 +3,7 @@
 
 #include <mutex>
 
+#include "eight_bit.h"
 #include "svdc_internal.h"
 
 using namespace svdc;
@@ -30,6 +31,23 @@ int32_t check_shape(const svdc_shape* s) {
   if (s->block_stride < (int64_t)(s->N - 1) * s->ldf + s->D || s->block_stride > kMaxElems / s->B) return SVDC_E_SHAPE;
   const int64_t unit = s->dtype == SVDC_BF16 ? 8 : 4;
   if (s->D % unit || s->ldf % unit || s->block_stride % unit) return SVDC_E_ALIGN;
+  return SVDC_OK;
+}
+
+// Limits of the operators in 8 bits: rows and row strides (a stride is checked where its tensor is given)
+constexpr int32_t kMaxColumns8 = 1 << 20, kMaxOutputs8 = 1 << 24;
+bool rows8_ok(int64_t rows, int32_t D) { return rows >= 0 && rows <= INT32_MAX && D >= 1 && D <= kMaxColumns8; }
+bool stride8_ok(int64_t rows, int32_t D, int64_t ld) { return ld >= D && ld <= (int64_t(1) << 48) / (rows > 0 ? rows : 1); }
+bool plain_dtype(int32_t dtype) { return dtype == SVDC_F32 || dtype == SVDC_BF16; }
+size_t dtype_size(int32_t dtype) { return dtype == SVDC_F32 ? 4 : dtype == SVDC_BF16 ? 2 : 1; }
+
+int32_t check_matmul8(const svdc_matmul8* p) {
+  if (!p) return SVDC_E_NULL;
+  if (!plain_dtype(p->dtype) && p->dtype != SVDC_E4M3) return SVDC_E_DTYPE;
+  if (p->act != SVDC_ACT_NONE && p->act != SVDC_ACT_GELU && p->act != SVDC_ACT_SWIGLU) return SVDC_E_PARAM;
+  if (!rows8_ok(p->M, p->K) || p->N < 1 || p->N > kMaxOutputs8) return SVDC_E_SHAPE;
+  if (p->dtype != SVDC_E4M3 && !stride8_ok(p->M, p->N, p->ldo)) return SVDC_E_SHAPE;
+  if (p->dtype == SVDC_E4M3 && p->N > kMaxColumns8) return SVDC_E_SHAPE;   // the result is a matrix in 8 bits itself
   return SVDC_OK;
 }
 
@@ -329,6 +347,64 @@ int32_t svdcache_basis_similarity(const svdc_shape* shape, const float* V_a, con
   if (!V_a || !V_b || !sim_dir) return SVDC_E_NULL;
   if (sim_sigma && (!sigma_a || !sigma_b)) return SVDC_E_NULL;
   return launch_basis_similarity(*shape, V_a, sigma_a, V_b, sigma_b, sim_dir, sim_sigma, (hipStream_t)stream);
+}
+
+size_t svdcache_q8_bytes(int64_t rows, int32_t D) {
+  return rows8_ok(rows, D) ? (size_t)(rows * q8_row_bytes(D)) : 0;
+}
+
+size_t svdcache_q8_scale_bytes(int64_t rows, int32_t D, int32_t block_rows) {
+  if (!rows8_ok(rows, D) || (block_rows != 1 && block_rows != kScaleBlock)) return 0;
+  return (size_t)((rows + block_rows - 1) / block_rows * q8_scale_row_bytes(D));
+}
+
+int32_t svdcache_rms_norm8(const svdc_norm8* p, const void* X, const void* F, const float* gain, void* H, void* Y, void* Q, void* scales,
+                           void* stream) {
+  if (!p) return SVDC_E_NULL;
+  if (!plain_dtype(p->dtype) || (F && !plain_dtype(p->dtype_f))) return SVDC_E_DTYPE;
+  if (!(p->eps >= 0.f && p->eps <= 3.402823466e38f)) return SVDC_E_PARAM;
+  if (!rows8_ok(p->rows, p->D) || !stride8_ok(p->rows, p->D, p->ldx) || (F && !stride8_ok(p->rows, p->D, p->ldf)) ||
+      (H && !stride8_ok(p->rows, p->D, p->ldh)) || (Y && !stride8_ok(p->rows, p->D, p->ldy)))
+    return SVDC_E_SHAPE;
+  if (p->rows == 0) return SVDC_OK;
+  if (!X || (!Y && !Q) || (Q == nullptr) != (scales == nullptr)) return SVDC_E_NULL;
+  const size_t unit = dtype_size(p->dtype);
+  if (!aligned(X, unit) || (F && !aligned(F, dtype_size(p->dtype_f))) || (gain && !aligned(gain, 4)) || (H && !aligned(H, unit)) ||
+      (Y && !aligned(Y, unit)) || (Q && !aligned(Q, 16)) || (scales && !aligned(scales, 4)))
+    return SVDC_E_ALIGN;
+  // a row is written where another one is still read, if the buffers are the same and the strides are not
+  if (H && ((H == X && p->ldh != p->ldx) || (F && H == F && (p->ldh != p->ldf || p->dtype != p->dtype_f)))) return SVDC_E_PARAM;
+  if (Y && (Y == X || Y == F || Y == H)) return SVDC_E_PARAM;
+  return launch_rms_norm8(*p, X, F, gain, H, Y, Q, scales, (hipStream_t)stream);
+}
+
+int32_t svdcache_quantize8(const svdc_quant8* p, const void* X, void* Q, void* scales, void* stream) {
+  if (!p) return SVDC_E_NULL;
+  if (!plain_dtype(p->dtype)) return SVDC_E_DTYPE;
+  if ((p->block_rows != 1 && p->block_rows != kScaleBlock) || p->reserved != 0) return SVDC_E_PARAM;
+  if (!rows8_ok(p->rows, p->D) || !stride8_ok(p->rows, p->D, p->ldx)) return SVDC_E_SHAPE;
+  if (p->rows == 0) return SVDC_OK;
+  if (!X || !Q || !scales) return SVDC_E_NULL;
+  if (!aligned(X, dtype_size(p->dtype)) || !aligned(Q, 16) || !aligned(scales, 4)) return SVDC_E_ALIGN;
+  return launch_quantize8(*p, X, Q, scales, (hipStream_t)stream);
+}
+
+size_t svdcache_matmul8_workspace_bytes(const svdc_matmul8* p) { return check_matmul8(p) == SVDC_OK ? matmul8_workspace_bytes(*p) : 0; }
+
+int32_t svdcache_matmul8(const svdc_matmul8* p, const void* A, const void* A_scales, const void* W, const void* W_scales, const float* bias,
+                         void* Out, void* Out_scales, void* workspace, size_t workspace_bytes, void* stream) {
+  const int32_t rc = check_matmul8(p);
+  if (rc != SVDC_OK) return rc;
+  if (p->M == 0) return SVDC_OK;
+  if (!A || !A_scales || !W || !W_scales || !Out || (p->dtype == SVDC_E4M3 && !Out_scales)) return SVDC_E_NULL;
+  if (!aligned(A, 16) || !aligned(A_scales, 4) || !aligned(W, 16) || !aligned(W_scales, 4) || (bias && !aligned(bias, 4)) ||
+      !aligned(Out, p->dtype == SVDC_E4M3 ? 16 : dtype_size(p->dtype)) || (p->dtype == SVDC_E4M3 && !aligned(Out_scales, 4)))
+    return SVDC_E_ALIGN;
+  const size_t need = matmul8_workspace_bytes(*p);
+  if (need && !workspace) return SVDC_E_NULL;
+  if (need && !aligned(workspace, 256)) return SVDC_E_ALIGN;
+  if (need > workspace_bytes) return SVDC_E_WORKSPACE;
+  return launch_matmul8(*p, A, A_scales, W, W_scales, bias, Out, Out_scales, need ? workspace : nullptr, (hipStream_t)stream);
 }
 
 }  // extern "C"
