@@ -4,6 +4,9 @@
 
 namespace svdc {
 
+// 16 bytes aligned to the smallest element: global memory takes wide accesses at any such address
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
 constexpr int kScaleBlock = 128;   // columns (and, for weights, rows) that share a scale
 
 __host__ __device__ inline int q8_blocks(int D) { return (D + kScaleBlock - 1) / kScaleBlock; }

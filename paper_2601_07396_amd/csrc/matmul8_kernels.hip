@@ -10,6 +10,7 @@
 // float32.  That is about 4e-5 of a result: nothing beside the rounding of a result to bfloat16 or e4m3, but not float32.  Results in float32 are made with
 // bfloat16 instructions, at half the rate: e4m3 values times powers of two are bfloat16 values exactly, and those products are summed with 24 bits.
 #include <algorithm>
+#include <type_traits>
 
 #include "eight_bit.h"
 #include "svdc_internal.h"
@@ -135,14 +136,339 @@ __global__ __launch_bounds__(512) void matmul8_kernel(MatmulArgs a) {
   }
 }
 
+// ---- tiles ----------------------------------------------------------------------------------------------------------
+//
+// A workgroup of four waves makes BM = 64 TM rows by BN = 64 TN rows of W; a wave 32 TM by 32 TN of them, with 32 x 32 x 64 instructions (the same rate as
+// 16 x 16 x 128, half the operand words).  Two stages of 128 columns of both operands lie in LDS, written by direct loads one block ahead; a wave's operands
+// lie in two register sets, one read from LDS while the other is multiplied.  Rows of 128 bytes are eight 16-byte slots; slot s of row r holds columns
+// 16 (s ^ swizzle(r)): eight consecutive rows and the rows of one parity of sixteen have different slots of a column, so that reads meet no bank twice.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }   // a value that all lanes hold, as a scalar
+__device__ __forceinline__ int swizzle(int row) { return (row & 7) ^ (row >> 3 & 1); }
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <bool EXACT>
+__device__ __forceinline__ void product32(f32x16& c, const i32x8& w, const i32x8& a, int sw, int sa) {
+  if (!EXACT) {
+    c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, a, c, 0, 0, 0, sw, 0, sa);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(w[2 * i], w[2 * i + 1], sw & 255), widen8(a[2 * i], a[2 * i + 1], sa & 255), c, 0, 0, 0);
+  }
+}
+
+// Writes 16 bytes of Out, ES bytes an element, from column col on; `n` elements are in range
+template <int ES>
+__device__ __forceinline__ void store16(void* Out, int64_t at, int n, const u32x4& v) {
+  if (n >= 16 / ES) {
+    *reinterpret_cast<u32x4_any*>(static_cast<uint8_t*>(Out) + at * ES) = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16 / ES; ++i) {
+      if (i >= n) break;
+      if (ES == 4) static_cast<uint32_t*>(Out)[at + i] = v[i];
+      if (ES == 2) static_cast<uint16_t*>(Out)[at + i] = (uint16_t)(v[i / 2] >> 16 * (i % 2));
+    }
+  }
+}
+
+// A wave's finished sums c[i][j][4 q + e] = Out[row 32 j + lane % 32][column 32 i + 8 q + 4 (lane / 32) + e], columns of i < TO, go to memory through its own
+// part of LDS, 128 bytes a row at most at a time, so that a wave writes whole lines.  inv: of the scales, for 8 bits.
+template <int TM, int TO, int ES, typename Acc>
+__device__ __forceinline__ void store_wave(const MatmulArgs& a, const Acc& c, int64_t m_first, int col_first, int lane, const float (&inv)[TM],
+                                           uint8_t* lds) {
+  constexpr int G = TO < 4 / ES ? TO : 4 / ES, RB = G * 32 * ES, CH = RB / 16, PER = 64 / CH;
+  const int r = lane % 32, h = lane / 32;
+  const int64_t ldo = ES == 1 ? q8_row_bytes(a.N) : a.ldo;
+  const int end = ES == 1 ? (int)q8_row_bytes(a.N) : a.N;
+#pragma unroll
+  for (int first = 0; first < TO; first += G) {
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int row = 32 * j + r, byte = (32 * g + 8 * q + 4 * h) * ES;
+          uint8_t* to = lds + row * RB + (byte / 16 ^ (row & (CH - 1))) * 16 + byte % 16;
+          const auto& t = c[first + g][j];
+          if (ES == 4) {
+            *reinterpret_cast<f32x4*>(to) = f32x4{t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
+          } else if (ES == 2) {
+            *reinterpret_cast<uint2*>(to) = uint2{pack_bf16(t[4 * q], t[4 * q + 1]), pack_bf16(t[4 * q + 2], t[4 * q + 3])};
+          } else {
+            *reinterpret_cast<uint32_t*>(to) = pack_e4m3(t[4 * q] * inv[j], t[4 * q + 1] * inv[j], t[4 * q + 2] * inv[j], t[4 * q + 3] * inv[j]);
+          }
+        }
+    asm volatile("" ::: "memory");         // a wave's LDS operations are carried out in order
+#pragma unroll
+    for (int p = 0; p < 32 * TM / PER; ++p) {
+      const int row = p * PER + lane / CH, chunk = lane % CH;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(lds + row * RB + (chunk ^ (row & (CH - 1))) * 16);
+      const int col = col_first + 32 * first + chunk * 16 / ES;
+      if (m_first + row < a.M && col < end) store16<ES>(a.Out, (m_first + row) * ldo + col, end - col, v);
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
+// Bias and activation on a wave's sums, the result in c[0 .. TO - 1]; gated: c[TO + i] is what c[i] gates
+template <int TM, int TN, int ACT, typename Acc>
+__device__ __forceinline__ void finish_wave(const MatmulArgs& a, Acc& c, int col_first, int h) {
+  constexpr bool GATED = ACT == SVDC_ACT_SWIGLU;
+  constexpr int TO = GATED ? TN / 2 : TN;
+#pragma unroll
+  for (int i = 0; i < TO; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int col = col_first + 32 * i + 8 * q + 4 * h;
+      float b[4], bu[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        b[e] = a.bias && col + e < a.N ? a.bias[col + e] : 0.f;
+        bu[e] = GATED && a.bias && col + e < a.N ? a.bias[a.N + col + e] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < TM; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float z = c[i][j][4 * q + e] + b[e];
+          if (GATED) z = silu(z) * (c[TO + i][j][4 * q + e] + bu[e]);
+          if (ACT == SVDC_ACT_GELU) z = gelu(z);
+          c[i][j][4 * q + e] = col + e < a.N ? z : 0.f;
+        }
+    }
+}
+
+// lds: 4096 TM bytes a wave; part: 4 * 32 TM floats.  Called by all waves of the workgroup.
+template <int TM, int TN, bool EXACT, bool GATED, typename Acc>
+__device__ __forceinline__ void store_tile(const MatmulArgs& a, Acc& c, int64_t m0, int n0, bool last, int wm, int wn, int lane, uint8_t* lds,
+                                           float* part) {
+  constexpr int TO = GATED ? TN / 2 : TN;
+  const int64_t m_first = m0 + wm * 32 * TM;
+  const int col_first = n0 + wn * 32 * TO;
+  uint8_t* mine = lds + (wn * 2 + wm) * 4096 * TM;
+  if (GATED)
+    finish_wave<TM, TN, SVDC_ACT_SWIGLU>(a, c, col_first, lane / 32);
+  else if (a.act == SVDC_ACT_GELU)
+    finish_wave<TM, TN, SVDC_ACT_GELU>(a, c, col_first, lane / 32);
+  else
+    finish_wave<TM, TN, SVDC_ACT_NONE>(a, c, col_first, lane / 32);
+  float inv[TM] = {};
+  if (EXACT) {
+    store_wave<TM, TO, 4>(a, c, m_first, col_first, lane, inv, mine);
+  } else if (a.dtype == SVDC_BF16) {
+    store_wave<TM, TO, 2>(a, c, m_first, col_first, lane, inv, mine);
+  } else if (TO >= 2) {
+    constexpr bool SHARED = TO < 4;        // the two waves of the columns share their scales
+    float top[TM];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      top[j] = 0.f;
+#pragma unroll
+      for (int i = 0; i < TO; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top[j] = fmaxf(top[j], fabsf(c[i][j][e]));
+      top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
+    }
+    if (SHARED) {
+#pragma unroll
+      for (int j = 0; j < TM; ++j) part[(wn * 2 + wm) * 32 * TM + 32 * j + lane % 32] = top[j];
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < TM; ++j) top[j] = fmaxf(top[j], part[((wn ^ 1) * 2 + wm) * 32 * TM + 32 * j + lane % 32]);
+    }
+    const int block = SHARED ? n0 / kScaleBlock : col_first / kScaleBlock, blocks = q8_blocks(a.N), row_bytes = q8_scale_row_bytes(a.N);
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int byte = scale_byte(top[j]);
+      inv[j] = inverse_scale(byte);
+      const int64_t m = m_first + 32 * j + lane;
+      if (lane < 32 && m < a.M) {
+        uint8_t* to = a.Os + m * row_bytes;
+        if (block < blocks && !(SHARED && wn)) to[block] = (uint8_t)byte;
+        if (last && wn)
+          for (int b = blocks; b < row_bytes; ++b) to[b] = 127;
+      }
+    }
+    store_wave<TM, TO, 1>(a, c, m_first, col_first, lane, inv, mine);
+  }
+}
+
+// An instruction is issued here and not where the compiler would move it, with its sums in accumulation registers
+__device__ __forceinline__ void hold(f32x16& c) {
+  asm volatile("" : "+a"(c));
+}
+
+template <int TM, int TN>
+struct TileStage {
+  __align__(1024) uint8_t b[64 * (TM + TN) * 128];
+};
+
+template <int TM, int TN, bool EXACT, bool GATED>
+__device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
+  constexpr int BM = 64 * TM, BN = 64 * TN, LOADS = (BM + BN) / 32;
+  __shared__ TileStage<TM, TN> stage0;
+  __shared__ TileStage<TM, TN> stage1;
+  const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int wm = wave & 1, wn = wave >> 1;
+  constexpr bool gated = GATED;
+  const int64_t Kp = q8_row_bytes(a.K);
+  const int blocks = uniform(q8_blocks(a.K)), ss = uniform(q8_scale_row_bytes(a.K));
+  const int columns = gated ? BN / 2 : BN;                  // of Out
+  const int column_tiles = (a.N + columns - 1) / columns;
+  const int row_tile = uniform(blockIdx.x / column_tiles), column_tile = uniform(blockIdx.x % column_tiles);
+  const int64_t m0 = (int64_t)row_tile * BM;
+  const int n0 = column_tile * columns;
+
+  // row of W behind row i of the tile; rows beyond the last are read as the last one, and what they give is not stored.  Gated: a wave's first 16 TN
+  // rows are gates, its others what they multiply
+  const auto w_row = [&](int i) {
+    if (!gated) return (int64_t)min(n0 + i, a.N - 1);
+    const int w = i / (32 * TN), j = i % (32 * TN), up = j / (16 * TN);
+    return (int64_t)min(n0 + w * 16 * TN + j % (16 * TN), a.N - 1) + (up ? a.N : 0);
+  };
+  const auto a_row = [&](int i) { return min(m0 + i, a.M - 1); };
+
+  // This wave's pieces of 8 rows of a stage: bounds-checked loads from A, the gates and what they multiply, each from the tile's first row on
+  const auto rows_of = [](const uint8_t* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, bytes, 0x00027000); };
+  const int a_bytes = uniform((int)(min<int64_t>(BM, a.M - m0) * Kp)), w_bytes = uniform((int)(min(columns, a.N - n0) * Kp));
+  const int64_t u_first = (gated ? (int64_t)a.N : 0) + n0;
+  const auto A1 = rows_of(a.A + m0 * Kp, a_bytes), W1 = rows_of(a.W + n0 * Kp, w_bytes), U1 = rows_of(a.W + u_first * Kp, w_bytes);
+  const auto is_up = [](int j) { return GATED && (j * 32 - BM) % (32 * TN) >= 16 * TN; };
+  uint32_t from[LOADS];
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j) {
+    const int i = (j * 4 + wave) * 8 + lane / 8, slot = (lane % 8) ^ swizzle(i);
+    from[j] = (uint32_t)((j * 32 < BM ? a_row(i) - m0 : w_row(i - BM) - n0 - (is_up(j) ? a.N : 0)) * Kp + slot * 16);
+  }
+  const auto load = [&](int j, int b, uint8_t* stage, __amdgpu_buffer_rsrc_t A, __amdgpu_buffer_rsrc_t W, __amdgpu_buffer_rsrc_t U) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(j * 32 < BM ? A : is_up(j) ? U : W, stage + (j * 4 + wave) * 1024, 16, from[j], uniform(b * 128), 0, 0);
+  };
+
+  const int r = lane % 32, h = lane / 32;
+  const int f = swizzle(r);
+  const int slot[4] = {((2 * h) ^ f) * 16, ((2 * h + 1) ^ f) * 16, ((4 + 2 * h) ^ f) * 16, ((5 + 2 * h) ^ f) * 16};
+  const int a_base = (wm * 32 * TM + r) * 128, w_base = (BM + wn * 32 * TN + r) * 128;
+  const auto operand = [&](const uint8_t* stage, int t, int half) {       // t < TN: of W, else of A
+    const uint8_t* row = stage + (t < TN ? w_base + t * 4096 : a_base + (t - TN) * 4096);
+    const u32x4 lo = *reinterpret_cast<const u32x4*>(row + slot[2 * half]), hi = *reinterpret_cast<const u32x4*>(row + slot[2 * half + 1]);
+    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  };
+
+  // scales of four blocks at a time, those of the current block in the lowest byte
+  const auto As = rows_of(a.As + m0 * ss, uniform((int)min<int64_t>(BM, a.M - m0) * ss)), Ws = rows_of(a.Ws, uniform(q8_blocks(gated ? 2 * a.N : a.N) * ss));
+  uint32_t scale_row[TN + TM];
+#pragma unroll
+  for (int t = 0; t < TN; ++t) scale_row[t] = (uint32_t)(w_row(wn * 32 * TN + t * 32 + r) / kScaleBlock * ss);
+#pragma unroll
+  for (int t = 0; t < TM; ++t) scale_row[TN + t] = (uint32_t)((a_row(wm * 32 * TM + t * 32 + r) - m0) * ss);
+  int sc[TN + TM], next_sc[TN + TM];
+  const auto load_scales = [&](int b, int* s) {
+#pragma unroll
+    for (int t = 0; t < TN + TM; ++t) s[t] = __builtin_amdgcn_raw_buffer_load_b32(t < TN ? Ws : As, scale_row[t], b, 0);
+  };
+
+  f32x16 c[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) c[i][j][k] = 0.f;
+  i32x8 x[2][TN + TM];
+
+  load_scales(0, sc);
+  load_scales(min(4, ss - 4), next_sc);
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j) load(j, 0, stage0.b, A1, W1, U1);
+  if (blocks > 1) {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) load(j, 1, stage1.b, A1, W1, U1);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < TN + TM; ++t) x[0][t] = operand(stage0.b, t, 0);
+
+  const auto multiply = [&](const i32x8* y, auto&& between) {
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j) {
+        between(i * TM + j);
+        product32<EXACT>(c[i][j], y[i], y[TN + j], sc[i], sc[TN + j]);
+        hold(c[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  };
+  // block b lies in `now` with its first half in x[0]; loads block b + 2 there (beyond the last one the loads are out of bounds and fetch nothing)
+  const auto block = [&](int b, uint8_t* now, uint8_t* then) {
+    multiply(x[0], [&](int t) {
+      if (t < TN + TM) x[1][t] = operand(now, t, 1);
+    });
+    asm volatile("s_waitcnt lgkmcnt(0) vmcnt(0)\n\ts_barrier" ::: "memory");
+    const int more = b + 2 < blocks ? -1 : 0;
+    const auto A2 = rows_of(a.A + m0 * Kp, a_bytes & more), W2 = rows_of(a.W + n0 * Kp, w_bytes & more), U2 = rows_of(a.W + u_first * Kp, w_bytes & more);
+    multiply(x[1], [&](int t) {
+      if (t < TN + TM) x[0][t] = operand(then, t, 0);
+#pragma unroll
+      for (int j = t * LOADS / (TN * TM); j < (t + 1) * LOADS / (TN * TM); ++j) load(j, b + 2, now, A2, W2, U2);
+    });
+    if ((b & 3) == 3) {
+#pragma unroll
+      for (int t = 0; t < TN + TM; ++t) sc[t] = next_sc[t];
+      load_scales(min(b + 5, ss - 4), next_sc);
+    } else {
+#pragma unroll
+      for (int t = 0; t < TN + TM; ++t) sc[t] = (int)((uint32_t)sc[t] >> 8);
+    }
+  };
+  int b = 0;
+  for (; b + 1 < blocks; b += 2) {
+    block(b, stage0.b, stage1.b);
+    block(b + 1, stage1.b, stage0.b);
+  }
+  if (b < blocks) block(b, stage0.b, stage1.b);
+  asm volatile("s_waitcnt lgkmcnt(0) vmcnt(0)\n\ts_barrier" ::: "memory");
+  store_tile<TM, TN, EXACT, GATED>(a, c, m0, n0, column_tile == column_tiles - 1, wm, wn, lane, stage0.b, reinterpret_cast<float*>(stage1.b));
+}
+
+template <int TM, int TN, bool EXACT, bool GATED>
+__global__ __launch_bounds__(256) void matmul8_tile_kernel(MatmulArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__          // buffer descriptors and accumulation registers mean nothing to the host's pass
+  tile_of_product<TM, TN, EXACT, GATED>(a);
+#endif
+}
+
 }  // namespace
 
 size_t matmul8_workspace_bytes(const svdc_matmul8&) { return 0; }
+
+namespace {
+
+template <int TM, int TN, bool EXACT, bool GATED>
+void launch_tiles(const MatmulArgs& a, hipStream_t st) {
+  const int columns = GATED ? 32 * TN : 64 * TN;
+  const int64_t tiles = (a.M + 64 * TM - 1) / (64 * TM) * ((a.N + columns - 1) / columns);
+  matmul8_tile_kernel<TM, TN, EXACT, GATED><<<(unsigned)tiles, 256, 0, st>>>(a);
+}
+
+}  // namespace
 
 int32_t launch_matmul8(const svdc_matmul8& p, const void* A, const void* As, const void* W, const void* Ws, const float* bias, void* Out, void* Os,
                        void*, hipStream_t st) {
   const MatmulArgs a{static_cast<const uint8_t*>(A), static_cast<const uint8_t*>(As), static_cast<const uint8_t*>(W), static_cast<const uint8_t*>(Ws),
                      bias, Out, static_cast<uint8_t*>(Os), p.M, p.ldo, p.N, p.K, p.dtype, p.act};
+  if (p.M >= 64) {
+    const bool gated = p.act == SVDC_ACT_SWIGLU, exact = p.dtype == SVDC_F32;
+    if (exact)
+      gated ? launch_tiles<2, 2, true, true>(a, st) : launch_tiles<2, 2, true, false>(a, st);
+    else
+      gated ? launch_tiles<4, 4, false, true>(a, st) : launch_tiles<4, 4, false, false>(a, st);
+    return launch_status();
+  }
   const int64_t tiles = (p.M + 15) / 16 * q8_blocks(p.N);
   const unsigned grid = (unsigned)std::min<int64_t>(tiles, 1 << 20);
   if (p.dtype == SVDC_F32)

@@ -12,11 +12,7 @@ namespace svdc {
 
 namespace {
 
-// 8 consecutive elements as float32, the first `n` of them in range (n may be <= 0 or above 8); zeros beyond.  The pointer is aligned to its
-// elements only: global memory takes wide loads at any such address.
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-
+// 8 consecutive elements as float32, the first `n` of them in range (n may be <= 0 or above 8); zeros beyond.  The pointer is aligned to its elements only.
 __device__ __forceinline__ void load8(const bf16_t* p, int n, float (&v)[8]) {
   if (n >= 8) {
     const u32x4_any w = *reinterpret_cast<const u32x4_any*>(p);
