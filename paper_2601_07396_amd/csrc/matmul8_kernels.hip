@@ -57,8 +57,13 @@ __device__ __forceinline__ f32x4 product(const i32x8& w, const i32x8& a, f32x4 c
   return c;
 }
 
-__device__ __forceinline__ float gelu(float x) { return x / (1.f + __expf(-1.5957691216057308f * (x + 0.044715f * x * x * x))); }
-__device__ __forceinline__ float silu(float x) { return x / (1.f + __expf(-x)); }
+// x / (1 + exp(-t)), with the hardware's power of two and reciprocal (one step of the last place each): half the instructions of a division
+__device__ __forceinline__ float times_sigmoid(float x, float t_log2e) {
+  return x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-t_log2e));
+}
+__device__ __forceinline__ float silu(float x) { return times_sigmoid(x, 1.4426950408889634f * x); }
+// with t = 2 sqrt(2 / pi) (x + 0.044715 x^3)
+__device__ __forceinline__ float gelu(float x) { return times_sigmoid(x, x * __builtin_fmaf(0.10294324f, x * x, 2.3022082f)); }
 
 // 8 waves: 128 columns of Out for 16 rows, a wave 16 columns of them (and the 16 they gate).
 template <bool EXACT>
@@ -158,6 +163,11 @@ __device__ __forceinline__ void product32(f32x16& c, const i32x8& w, const i32x8
   }
 }
 
+// An instruction is issued here and not where the compiler would move it, with its sums in accumulation registers
+__device__ __forceinline__ void hold(f32x16& c) {
+  asm volatile("" : "+a"(c));
+}
+
 // Writes 16 bytes of Out, ES bytes an element, from column col on; `n` elements are in range
 template <int ES>
 __device__ __forceinline__ void store16(void* Out, int64_t at, int n, const u32x4& v) {
@@ -173,132 +183,96 @@ __device__ __forceinline__ void store16(void* Out, int64_t at, int n, const u32x
   }
 }
 
-// A wave's finished sums c[i][j][4 q + e] = Out[row 32 j + lane % 32][column 32 i + 8 q + 4 (lane / 32) + e], columns of i < TO, go to memory through its own
-// part of LDS, 128 bytes a row at most at a time, so that a wave writes whole lines.  inv: of the scales, for 8 bits.
-template <int TM, int TO, int ES, typename Acc>
-__device__ __forceinline__ void store_wave(const MatmulArgs& a, const Acc& c, int64_t m_first, int col_first, int lane, const float (&inv)[TM],
-                                           uint8_t* lds) {
-  constexpr int G = TO < 4 / ES ? TO : 4 / ES, RB = G * 32 * ES, CH = RB / 16, PER = 64 / CH;
+// A wave's finished 32 rows v[i][4 q + e] = Out[row lane % 32][column 32 i + 8 q + 4 (lane / 32) + e] go to memory through its own part of LDS, so that it writes
+// whole lines.  inv: of the scale of the lane's row, for 8 bits.
+template <int TO, int ES>
+__device__ __forceinline__ void store_rows(const MatmulArgs& a, const float (&v)[TO][16], int64_t m_first, int col_first, int lane, float inv, uint8_t* lds) {
+  constexpr int RB = TO * 32 * ES, CH = RB / 16, PER = 64 / CH;
+  static_assert(RB <= 256, "");
   const int r = lane % 32, h = lane / 32;
   const int64_t ldo = ES == 1 ? q8_row_bytes(a.N) : a.ldo;
   const int end = ES == 1 ? (int)q8_row_bytes(a.N) : a.N;
 #pragma unroll
-  for (int first = 0; first < TO; first += G) {
-#pragma unroll
-    for (int j = 0; j < TM; ++j)
-#pragma unroll
-      for (int g = 0; g < G; ++g)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int row = 32 * j + r, byte = (32 * g + 8 * q + 4 * h) * ES;
-          uint8_t* to = lds + row * RB + (byte / 16 ^ (row & (CH - 1))) * 16 + byte % 16;
-          const auto& t = c[first + g][j];
-          if (ES == 4) {
-            *reinterpret_cast<f32x4*>(to) = f32x4{t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
-          } else if (ES == 2) {
-            *reinterpret_cast<uint2*>(to) = uint2{pack_bf16(t[4 * q], t[4 * q + 1]), pack_bf16(t[4 * q + 2], t[4 * q + 3])};
-          } else {
-            *reinterpret_cast<uint32_t*>(to) = pack_e4m3(t[4 * q] * inv[j], t[4 * q + 1] * inv[j], t[4 * q + 2] * inv[j], t[4 * q + 3] * inv[j]);
-          }
-        }
-    asm volatile("" ::: "memory");         // a wave's LDS operations are carried out in order
-#pragma unroll
-    for (int p = 0; p < 32 * TM / PER; ++p) {
-      const int row = p * PER + lane / CH, chunk = lane % CH;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(lds + row * RB + (chunk ^ (row & (CH - 1))) * 16);
-      const int col = col_first + 32 * first + chunk * 16 / ES;
-      if (m_first + row < a.M && col < end) store16<ES>(a.Out, (m_first + row) * ldo + col, end - col, v);
-    }
-    asm volatile("" ::: "memory");
-  }
-}
-
-// Bias and activation on a wave's sums, the result in c[0 .. TO - 1]; gated: c[TO + i] is what c[i] gates
-template <int TM, int TN, int ACT, typename Acc>
-__device__ __forceinline__ void finish_wave(const MatmulArgs& a, Acc& c, int col_first, int h) {
-  constexpr bool GATED = ACT == SVDC_ACT_SWIGLU;
-  constexpr int TO = GATED ? TN / 2 : TN;
-#pragma unroll
   for (int i = 0; i < TO; ++i)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int col = col_first + 32 * i + 8 * q + 4 * h;
-      float b[4], bu[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        b[e] = a.bias && col + e < a.N ? a.bias[col + e] : 0.f;
-        bu[e] = GATED && a.bias && col + e < a.N ? a.bias[a.N + col + e] : 0.f;
-      }
-#pragma unroll
-      for (int j = 0; j < TM; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float z = c[i][j][4 * q + e] + b[e];
-          if (GATED) z = silu(z) * (c[TO + i][j][4 * q + e] + bu[e]);
-          if (ACT == SVDC_ACT_GELU) z = gelu(z);
-          c[i][j][4 * q + e] = col + e < a.N ? z : 0.f;
-        }
+      const int byte = (32 * i + 8 * q + 4 * h) * ES;
+      uint8_t* to = lds + r * RB + (byte / 16 ^ (r & (CH - 1))) * 16 + byte % 16;
+      const float *t = v[i] + 4 * q;
+      if (ES == 4)
+        *reinterpret_cast<f32x4*>(to) = f32x4{t[0], t[1], t[2], t[3]};
+      else if (ES == 2)
+        *reinterpret_cast<uint2*>(to) = uint2{pack_bf16(t[0], t[1]), pack_bf16(t[2], t[3])};
+      else
+        *reinterpret_cast<uint32_t*>(to) = pack_e4m3(t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv);
     }
+  asm volatile("" ::: "memory");           // a wave's LDS operations are carried out in order
+#pragma unroll
+  for (int p = 0; p < 32 / PER; ++p) {
+    const int row = p * PER + lane / CH, chunk = lane % CH;
+    const u32x4 w = *reinterpret_cast<const u32x4*>(lds + row * RB + (chunk ^ (row & (CH - 1))) * 16);
+    const int col = col_first + chunk * 16 / ES;
+    if (m_first + row < a.M && col < end) store16<ES>(a.Out, (m_first + row) * ldo + col, end - col, w);
+  }
+  asm volatile("" ::: "memory");
 }
 
-// lds: 4096 TM bytes a wave; part: 4 * 32 TM floats.  Called by all waves of the workgroup.
-template <int TM, int TN, bool EXACT, bool GATED, typename Acc>
-__device__ __forceinline__ void store_tile(const MatmulArgs& a, Acc& c, int64_t m0, int n0, bool last, int wm, int wn, int lane, uint8_t* lds,
+// A wave's sums c (bias included; gated: c[TO + i] is what c[i] gates) to Out.  lds: 32 * 32 TO * 4 bytes a wave at most; part: 4 * 32 floats.  Called by all
+// waves of the workgroup.  edge: the tile reaches beyond column N.
+template <int TM, int TN, int ACT, int ES, typename Acc>
+__device__ __forceinline__ void store_tile(const MatmulArgs& a, Acc& c, int64_t m0, int n0, bool edge, int wm, int wn, int lane, uint8_t* lds,
                                            float* part) {
+  constexpr bool GATED = ACT == SVDC_ACT_SWIGLU;
   constexpr int TO = GATED ? TN / 2 : TN;
-  const int64_t m_first = m0 + wm * 32 * TM;
-  const int col_first = n0 + wn * 32 * TO;
-  uint8_t* mine = lds + (wn * 2 + wm) * 4096 * TM;
-  if (GATED)
-    finish_wave<TM, TN, SVDC_ACT_SWIGLU>(a, c, col_first, lane / 32);
-  else if (a.act == SVDC_ACT_GELU)
-    finish_wave<TM, TN, SVDC_ACT_GELU>(a, c, col_first, lane / 32);
-  else
-    finish_wave<TM, TN, SVDC_ACT_NONE>(a, c, col_first, lane / 32);
-  float inv[TM] = {};
-  if (EXACT) {
-    store_wave<TM, TO, 4>(a, c, m_first, col_first, lane, inv, mine);
-  } else if (a.dtype == SVDC_BF16) {
-    store_wave<TM, TO, 2>(a, c, m_first, col_first, lane, inv, mine);
-  } else if (TO >= 2) {
-    constexpr bool SHARED = TO < 4;        // the two waves of the columns share their scales
-    float top[TM];
+  constexpr bool SHARED = ES == 1 && TO < 4;        // the two waves of the columns share their scales
+  const int h = lane / 32, col_first = n0 + wn * 32 * TO;
+  uint8_t* mine = lds + (wn * 2 + wm) * (32 * 32 * TO * ES);
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      top[j] = 0.f;
+  for (int j = 0; j < TM; ++j) {
+    const int64_t m_first = m0 + wm * 32 * TM + 32 * j;
+#pragma unroll
+    for (int i = 0; i < TN; ++i) hold(c[i][j]);      // 32 rows after the other, not all in registers at once
+    float v[TO][16];
+#pragma unroll
+    for (int i = 0; i < TO; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float z = c[i][j][e];
+        v[i][e] = ACT == SVDC_ACT_GELU ? gelu(z) : GATED ? silu(z) * c[TO + i][j][e] : z;
+      }
+    float inv = 1.f;
+    if (ES == 1) {
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < TO; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (col_first + 32 * i + e / 4 * 8 + 4 * h + e % 4 >= a.N) v[i][e] = 0.f;
+      }
+      float top = 0.f;
 #pragma unroll
       for (int i = 0; i < TO; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top[j] = fmaxf(top[j], fabsf(c[i][j][e]));
-      top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
-    }
-    if (SHARED) {
-#pragma unroll
-      for (int j = 0; j < TM; ++j) part[(wn * 2 + wm) * 32 * TM + 32 * j + lane % 32] = top[j];
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < TM; ++j) top[j] = fmaxf(top[j], part[((wn ^ 1) * 2 + wm) * 32 * TM + 32 * j + lane % 32]);
-    }
-    const int block = SHARED ? n0 / kScaleBlock : col_first / kScaleBlock, blocks = q8_blocks(a.N), row_bytes = q8_scale_row_bytes(a.N);
-#pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int byte = scale_byte(top[j]);
-      inv[j] = inverse_scale(byte);
-      const int64_t m = m_first + 32 * j + lane;
-      if (lane < 32 && m < a.M) {
-        uint8_t* to = a.Os + m * row_bytes;
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(v[i][e]));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (SHARED) {
+        __syncthreads();                   // the maxima of the rows before have been read
+        part[(wn * 2 + wm) * 32 + lane % 32] = top;
+        __syncthreads();
+        top = fmaxf(top, part[((wn ^ 1) * 2 + wm) * 32 + lane % 32]);
+      }
+      const int byte = scale_byte(top);
+      inv = inverse_scale(byte);
+      const int block = (SHARED ? n0 : col_first) / kScaleBlock, blocks = q8_blocks(a.N), row_bytes = q8_scale_row_bytes(a.N);
+      if (lane < 32 && m_first + lane < a.M) {
+        uint8_t* to = a.Os + (m_first + lane) * row_bytes;
         if (block < blocks && !(SHARED && wn)) to[block] = (uint8_t)byte;
-        if (last && wn)
+        if (edge && wn)
           for (int b = blocks; b < row_bytes; ++b) to[b] = 127;
       }
     }
-    store_wave<TM, TO, 1>(a, c, m_first, col_first, lane, inv, mine);
+    store_rows<TO, ES>(a, v, m_first, col_first, lane, inv, mine);
   }
-}
-
-// An instruction is issued here and not where the compiler would move it, with its sums in accumulation registers
-__device__ __forceinline__ void hold(f32x16& c) {
-  asm volatile("" : "+a"(c));
 }
 
 template <int TM, int TN>
@@ -306,9 +280,20 @@ struct TileStage {
   __align__(1024) uint8_t b[64 * (TM + TN) * 128];
 };
 
-template <int TM, int TN, bool EXACT, bool GATED>
+// The tile of workgroup `id`.  Workgroups go round the eight dies in turn; each die gets a run of tiles of its own, in groups of eight rows of tiles, column
+// by column, so that the 32 at work on a die at a time share 8 + 4 operands of tiles in its cache.
+__device__ __forceinline__ void tile_at(int id, int row_tiles, int column_tiles, int& row, int& column) {
+  const int tiles = row_tiles * column_tiles, each = tiles / 8, more = tiles % 8, die = id % 8;
+  const int t = die * each + min(die, more) + id / 8;
+  const int group = t / (8 * column_tiles), first = group * 8, high = min(8, row_tiles - first), at = t - group * 8 * column_tiles;
+  row = uniform(first + at % high);
+  column = uniform(at / high);
+}
+
+template <int TM, int TN, int ACT, int ES>
 __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
-  constexpr int BM = 64 * TM, BN = 64 * TN, LOADS = (BM + BN) / 32;
+  constexpr bool EXACT = ES == 4, GATED = ACT == SVDC_ACT_SWIGLU;
+  constexpr int BM = 64 * TM, BN = 64 * TN, LOADS = (BM + BN) / 32, READ = TM * TN > 4 ? TN + TM + 1 : TN * TM - 1;
   __shared__ TileStage<TM, TN> stage0;
   __shared__ TileStage<TM, TN> stage1;
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -318,7 +303,9 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
   const int blocks = uniform(q8_blocks(a.K)), ss = uniform(q8_scale_row_bytes(a.K));
   const int columns = gated ? BN / 2 : BN;                  // of Out
   const int column_tiles = (a.N + columns - 1) / columns;
-  const int row_tile = uniform(blockIdx.x / column_tiles), column_tile = uniform(blockIdx.x % column_tiles);
+  const int row_tiles = (int)((a.M + BM - 1) / BM);
+  int row_tile, column_tile;
+  tile_at(blockIdx.x, row_tiles, column_tiles, row_tile, column_tile);
   const int64_t m0 = (int64_t)row_tile * BM;
   const int n0 = column_tile * columns;
 
@@ -370,13 +357,22 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
     for (int t = 0; t < TN + TM; ++t) s[t] = __builtin_amdgcn_raw_buffer_load_b32(t < TN ? Ws : As, scale_row[t], b, 0);
   };
 
+  // the sums start at the bias: bounds-checked loads, zero beyond the last column and without one
+  const uint8_t* const bias_bytes = reinterpret_cast<const uint8_t*>(a.bias);
+  const auto bias_z = rows_of(bias_bytes, uniform(a.bias ? a.N * 4 : 0)),
+             bias_u = rows_of(bias_bytes + (gated ? (int64_t)a.N * 4 : 0), uniform(a.bias ? a.N * 4 : 0));
   f32x16 c[TN][TM];
 #pragma unroll
-  for (int i = 0; i < TN; ++i)
+  for (int i = 0; i < TN; ++i) {
+    f32x16 bias;
 #pragma unroll
-    for (int j = 0; j < TM; ++j)
+    for (int e = 0; e < 16; ++e) {
+      const int col = n0 + wn * 32 * (gated ? TN / 2 : TN) + 32 * (gated ? i % (TN / 2) : i) + e / 4 * 8 + 4 * h + e % 4;
+      bias[e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(gated && i >= TN / 2 ? bias_u : bias_z, col * 4, 0, 0));
+    }
 #pragma unroll
-      for (int k = 0; k < 16; ++k) c[i][j][k] = 0.f;
+    for (int j = 0; j < TM; ++j) c[i][j] = bias;
+  }
   i32x8 x[2][TN + TM];
 
   load_scales(0, sc);
@@ -403,18 +399,22 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
         __builtin_amdgcn_sched_barrier(0);
       }
   };
-  // block b lies in `now` with its first half in x[0]; loads block b + 2 there (beyond the last one the loads are out of bounds and fetch nothing)
+  // Block b lies in `now` with its first half in x[0].  Once all waves have read its second half, block b + 2 is loaded there (beyond the last one the
+  // loads are out of bounds and fetch nothing); it has a block and a half's time to arrive.
   const auto block = [&](int b, uint8_t* now, uint8_t* then) {
-    multiply(x[0], [&](int t) {
-      if (t < TN + TM) x[1][t] = operand(now, t, 1);
-    });
-    asm volatile("s_waitcnt lgkmcnt(0) vmcnt(0)\n\ts_barrier" ::: "memory");
     const int more = b + 2 < blocks ? -1 : 0;
     const auto A2 = rows_of(a.A + m0 * Kp, a_bytes & more), W2 = rows_of(a.W + n0 * Kp, w_bytes & more), U2 = rows_of(a.W + u_first * Kp, w_bytes & more);
+    multiply(x[0], [&](int t) {
+      if (t < TN + TM) x[1][t] = operand(now, t, 1);
+      if (t == READ) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (t >= READ) {
+#pragma unroll
+        for (int j = (t - READ) * LOADS / (TN * TM - READ); j < (t - READ + 1) * LOADS / (TN * TM - READ); ++j) load(j, b + 2, now, A2, W2, U2);
+      }
+    });
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LOADS) : "memory");
     multiply(x[1], [&](int t) {
       if (t < TN + TM) x[0][t] = operand(then, t, 0);
-#pragma unroll
-      for (int j = t * LOADS / (TN * TM); j < (t + 1) * LOADS / (TN * TM); ++j) load(j, b + 2, now, A2, W2, U2);
     });
     if ((b & 3) == 3) {
 #pragma unroll
@@ -432,13 +432,15 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
   }
   if (b < blocks) block(b, stage0.b, stage1.b);
   asm volatile("s_waitcnt lgkmcnt(0) vmcnt(0)\n\ts_barrier" ::: "memory");
-  store_tile<TM, TN, EXACT, GATED>(a, c, m0, n0, column_tile == column_tiles - 1, wm, wn, lane, stage0.b, reinterpret_cast<float*>(stage1.b));
+  const bool edge = n0 + columns > a.N || column_tile == column_tiles - 1;
+  store_tile<TM, TN, ACT, ES>(a, c, m0, n0, edge, wm, wn, lane, stage0.b, reinterpret_cast<float*>(stage1.b));
 }
 
-template <int TM, int TN, bool EXACT, bool GATED>
+// ACT: svdc_act;  ES: bytes of an element of Out
+template <int TM, int TN, int ACT, int ES>
 __global__ __launch_bounds__(256) void matmul8_tile_kernel(MatmulArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__          // buffer descriptors and accumulation registers mean nothing to the host's pass
-  tile_of_product<TM, TN, EXACT, GATED>(a);
+  tile_of_product<TM, TN, ACT, ES>(a);
 #endif
 }
 
@@ -448,11 +450,21 @@ size_t matmul8_workspace_bytes(const svdc_matmul8&) { return 0; }
 
 namespace {
 
-template <int TM, int TN, bool EXACT, bool GATED>
+template <int TM, int TN, int ACT, int ES>
 void launch_tiles(const MatmulArgs& a, hipStream_t st) {
-  const int columns = GATED ? 32 * TN : 64 * TN;
+  const int columns = ACT == SVDC_ACT_SWIGLU ? 32 * TN : 64 * TN;
   const int64_t tiles = (a.M + 64 * TM - 1) / (64 * TM) * ((a.N + columns - 1) / columns);
-  matmul8_tile_kernel<TM, TN, EXACT, GATED><<<(unsigned)tiles, 256, 0, st>>>(a);
+  matmul8_tile_kernel<TM, TN, ACT, ES><<<(unsigned)tiles, 256, 0, st>>>(a);
+}
+
+template <int TM, int TN, int ES>
+void launch_tiles(const MatmulArgs& a, hipStream_t st) {
+  if (a.act == SVDC_ACT_SWIGLU)
+    launch_tiles<TM, TN, SVDC_ACT_SWIGLU, ES>(a, st);
+  else if (a.act == SVDC_ACT_GELU)
+    launch_tiles<TM, TN, SVDC_ACT_GELU, ES>(a, st);
+  else
+    launch_tiles<TM, TN, SVDC_ACT_NONE, ES>(a, st);
 }
 
 }  // namespace
@@ -462,11 +474,12 @@ int32_t launch_matmul8(const svdc_matmul8& p, const void* A, const void* As, con
   const MatmulArgs a{static_cast<const uint8_t*>(A), static_cast<const uint8_t*>(As), static_cast<const uint8_t*>(W), static_cast<const uint8_t*>(Ws),
                      bias, Out, static_cast<uint8_t*>(Os), p.M, p.ldo, p.N, p.K, p.dtype, p.act};
   if (p.M >= 64) {
-    const bool gated = p.act == SVDC_ACT_SWIGLU, exact = p.dtype == SVDC_F32;
-    if (exact)
-      gated ? launch_tiles<2, 2, true, true>(a, st) : launch_tiles<2, 2, true, false>(a, st);
+    if (p.dtype == SVDC_F32)
+      launch_tiles<2, 2, 4>(a, st);
+    else if (p.dtype == SVDC_BF16)
+      launch_tiles<4, 4, 2>(a, st);
     else
-      gated ? launch_tiles<4, 4, false, true>(a, st) : launch_tiles<4, 4, false, false>(a, st);
+      launch_tiles<4, 4, 1>(a, st);
     return launch_status();
   }
   const int64_t tiles = (p.M + 15) / 16 * q8_blocks(p.N);
