@@ -26,8 +26,9 @@ struct MatmulArgs {
   const float* bias;
   void* Out;
   uint8_t* Os;
+  float* partial;      // sums of parts of the columns of A and W, or nullptr
   int64_t M, ldo;
-  int N, K, dtype, act;
+  int N, K, dtype, act, splits;
 };
 
 __device__ __forceinline__ f32x4 mfma8(const i32x8& w, const i32x8& a, const f32x4& c, int sw, int sa) {
@@ -65,79 +66,226 @@ __device__ __forceinline__ float silu(float x) { return times_sigmoid(x, 1.44269
 // with t = 2 sqrt(2 / pi) (x + 0.044715 x^3)
 __device__ __forceinline__ float gelu(float x) { return times_sigmoid(x, x * __builtin_fmaf(0.10294324f, x * x, 2.3022082f)); }
 
-// 8 waves: 128 columns of Out for 16 rows, a wave 16 columns of them (and the 16 they gate).
-template <bool EXACT>
-__global__ __launch_bounds__(512) void matmul8_kernel(MatmulArgs a) {
-  __shared__ float part[8][16];
-  const int column_tiles = q8_blocks(a.N);
-  const int64_t tiles = (a.M + 15) / 16 * column_tiles;
-  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-  const int64_t row_tile = tile / column_tiles;
-  const int column_tile = (int)(tile - row_tile * column_tiles);
-  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
+// Column `col` of Out from its sum z (and the sum u that it gates); zero beyond the last column
+__device__ __forceinline__ float finished(const MatmulArgs& a, int col, float z, float u) {
+  if (col >= a.N) return 0.f;
+  if (a.bias) {
+    z += a.bias[col];
+    if (a.act == SVDC_ACT_SWIGLU) u += a.bias[a.N + col];
+  }
+  return a.act == SVDC_ACT_GELU ? gelu(z) : a.act == SVDC_ACT_SWIGLU ? silu(z) * u : z;
+}
+
+// ---- few rows, or few tiles ------------------------------------------------------------------------------------------
+//
+// Where there are not enough large tiles to occupy the card, a workgroup makes 16 TM rows by 16 TN columns and its eight waves share the blocks of columns of
+// A and W: wave w takes blocks w, w + 8, ... straight from memory into registers (nothing is used twice within a wave), and the eight sums are added through
+// LDS, always in the same order.  What it costs is the weights' bytes for few rows, and the operands' way out of L2 for many.
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }   // a value that all lanes hold, as a scalar
+
+// a buffer for bounds-checked accesses: loads beyond its end give zero
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t bounded(const void* p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, uniform((int)bytes), 0x00027000);
+}
+
+constexpr int kShareWaves = 8;
+
+// GATED: TN tiles of gates and TN of what they gate.  EXACT: float32 sums.  EIGHT: the result is in 8 bits (TN = 8).
+template <int TM, int TN, bool EXACT, bool GATED, bool EIGHT>
+__device__ __forceinline__ void shared_sums(const MatmulArgs& a) {
+  constexpr int NW = GATED ? 2 * TN : TN, COLUMNS = 16 * TN, ROWS = 16 * TM;
+  constexpr bool AHEAD = (TM + NW) * 16 + TM * NW * 4 + (EXACT ? 48 : 0) <= 200;   // registers for the operands of the next block too
+  __shared__ f32x4 sums[kShareWaves][NW * TM][kWave];
+  __shared__ float tops[TM * 16][8];
+  const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
   const int64_t Kp = q8_row_bytes(a.K);
-  const int blocks = q8_blocks(a.K), ss = q8_scale_row_bytes(a.K);
-  const int n0 = column_tile * 128 + wave * 16;
-  const int64_t m0 = row_tile * 16;
-  const int gated = a.act == SVDC_ACT_SWIGLU;
-  // rows beyond the last are read as the last one; what they give is not stored
-  const int n = min(n0 + r, a.N - 1);
-  const int64_t m = min(m0 + r, a.M - 1);
-  const uint8_t* A = a.A + m * Kp + 32 * g;
-  const uint8_t* As = a.As + m * ss;
-  const uint8_t* W = a.W + n * Kp + 32 * g;
-  const uint8_t* Ws = a.Ws + (int64_t)(n / kScaleBlock) * ss;
-  const int nu = a.N + n;
-  const uint8_t* U = a.W + nu * Kp + 32 * g;
-  const uint8_t* Us = a.Ws + (int64_t)(nu / kScaleBlock) * ss;
-  f32x4 z = {0.f, 0.f, 0.f, 0.f}, u = z;
-  for (int b = 0; b < blocks; ++b) {
-    const i32x8 x = load32(A + b * 128);
-    z = product<EXACT>(load32(W + b * 128), x, z, Ws[b], As[b]);
-    if (gated) u = product<EXACT>(load32(U + b * 128), x, u, Us[b], As[b]);
-  }
-  float v[4];
-  const int nt = n0 + 4 * g;
+  const int blocks = uniform(q8_blocks(a.K)), ss = uniform(q8_scale_row_bytes(a.K));
+  const int column_tiles = (a.N + COLUMNS - 1) / COLUMNS;
+  const int row_tile = uniform(blockIdx.x / column_tiles), column_tile = uniform(blockIdx.x % column_tiles);
+  const int64_t m0 = (int64_t)row_tile * ROWS;
+  const int n0 = column_tile * COLUMNS, rows = (int)min<int64_t>(ROWS, a.M - m0), columns = min(COLUMNS, a.N - n0);
+
+  const auto A = bounded(a.A + m0 * Kp, rows * Kp), W = bounded(a.W + n0 * Kp, columns * Kp),
+             U = bounded(a.W + ((GATED ? (int64_t)a.N : 0) + n0) * Kp, columns * Kp);
+  const auto As = bounded(a.As + m0 * ss, rows * ss), Ws = bounded(a.Ws, (int64_t)q8_blocks(GATED ? 2 * a.N : a.N) * ss);
+  // a lane's 32 bytes of a row are 16 from each half of a block, so that a load takes 64 bytes in a row
+  uint32_t at[TM + NW], scale_at[TM + NW];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bool in = nt + i < a.N;
-    v[i] = z[i] + (a.bias && in ? a.bias[nt + i] : 0.f);
-    if (gated) v[i] = silu(v[i]) * (u[i] + (a.bias && in ? a.bias[a.N + nt + i] : 0.f));
-    if (a.act == SVDC_ACT_GELU) v[i] = gelu(v[i]);
-    if (!in) v[i] = 0.f;
+  for (int t = 0; t < TM + NW; ++t) {
+    const int i = (t < TM ? t : (t - TM) % TN) * 16 + r, up = t >= TM + TN ? a.N : 0;
+    at[t] = (uint32_t)(i * Kp + 16 * g);
+    scale_at[t] = (uint32_t)(t < TM ? i * ss : (min(n0 + i, a.N - 1) + up) / kScaleBlock * ss);
   }
-  const int64_t mo = m0 + r;
-  if (a.dtype == SVDC_E4M3) {
-    float t = 0.f;
+  struct Operands {
+    i32x8 x[TM + NW];
+    int s[TM + NW];
+  };
+  const auto load = [&](int b, Operands& o) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t = fmaxf(t, fabsf(v[i]));
-    t = fmaxf(t, __shfl_xor(t, 16));
-    t = fmaxf(t, __shfl_xor(t, 32));
-    __syncthreads();                     // the maxima of the tile before have been read
-    if (g == 0) part[wave][r] = t;
+    for (int t = 0; t < TM + NW; ++t) {
+      const auto from = t < TM ? A : t < TM + TN ? W : U;
+      const auto lo = __builtin_amdgcn_raw_buffer_load_b128(from, at[t], uniform(b * 128), 0),
+                 hi = __builtin_amdgcn_raw_buffer_load_b128(from, at[t], uniform(b * 128 + 64), 0);
+      o.x[t] = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+      o.s[t] = __builtin_amdgcn_raw_buffer_load_b8(t < TM ? As : Ws, scale_at[t], uniform(b), 0);
+    }
+  };
+  f32x4 c[NW][TM] = {};
+  const auto multiply = [&](const Operands& o) {
+#pragma unroll
+    for (int i = 0; i < NW; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j) c[i][j] = product<EXACT>(o.x[TM + i], o.x[j], c[i][j], o.s[TM + i], o.s[j]);
+  };
+  const int each = (blocks + a.splits - 1) / a.splits, first = uniform(blockIdx.y * each), last = uniform(min(blocks, first + each));
+  if (AHEAD) {
+    Operands o[2];
+    int b = first + wave;
+    if (b < last) load(b, o[0]);
+    for (; b < last; b += 2 * kShareWaves) {
+      if (b + kShareWaves < last) load(b + kShareWaves, o[1]);
+      multiply(o[0]);
+      if (b + kShareWaves < last) {
+        if (b + 2 * kShareWaves < last) load(b + 2 * kShareWaves, o[0]);
+        multiply(o[1]);
+      }
+    }
+  } else {
+    for (int b = first + wave; b < last; b += kShareWaves) {
+      Operands o;
+      load(b, o);
+      multiply(o);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NW; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) sums[wave][i * TM + j][lane] = c[i][j];
+  __syncthreads();
+
+  // wave w finishes tiles w, w + 8, ... of 16 columns by 16 rows: lane (r, g) columns 4 g .. 4 g + 3 of row r
+  constexpr int TURNS = (TN * TM + kShareWaves - 1) / kShareWaves;
+  float v[TURNS][4];
+#pragma unroll
+  for (int turn = 0; turn < TURNS; ++turn) {
+    const int tile = turn * kShareWaves + wave, i = tile / TM, j = tile % TM;
+    if (TN * TM % kShareWaves && tile >= TN * TM) break;
+    f32x4 z = {}, u = {};
+#pragma unroll
+    for (int w = 0; w < kShareWaves; ++w) {
+      z += sums[w][tile][lane];
+      if (GATED) u += sums[w][TN * TM + tile][lane];
+    }
+    const int col = n0 + 16 * i + 4 * g;
+    const int64_t row = m0 + 16 * j + r;
+    if (a.partial) {
+      if (row < a.M) {
+        float* to = a.partial + ((int64_t)blockIdx.y * a.M + row) * a.N + col;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col + e < a.N) to[e] = z[e];
+      }
+      continue;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[turn][e] = finished(a, col + e, z[e], GATED ? u[e] : 0.f);
+    if (EIGHT) {
+      float top = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(v[turn][e]));
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (g == 0) tops[16 * j + r][i] = top;
+    } else if (row < a.M) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + e < a.N) {
+          if (EXACT)
+            static_cast<float*>(a.Out)[row * a.ldo + col + e] = v[turn][e];
+          else
+            static_cast<bf16_t*>(a.Out)[row * a.ldo + col + e] = (bf16_t)v[turn][e];
+        }
+    }
+  }
+  if (EIGHT) {
+    static_assert(!EIGHT || TN == 8, "");
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 8; ++w) t = fmaxf(t, part[w][r]);
-    const int byte = scale_byte(t);
-    const float inv = inverse_scale(byte);
-    if (mo < a.M) {
-      *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.Out) + mo * q8_row_bytes(a.N) + nt) =
-          pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-      uint8_t* os = a.Os + mo * q8_scale_row_bytes(a.N);
-      if (wave == 0 && g == 0) os[column_tile] = (uint8_t)byte;
-      if (wave == 1 && g == 0 && column_tile == column_tiles - 1)
-        for (int s = column_tiles; s < q8_scale_row_bytes(a.N); ++s) os[s] = 127;
-    }
-  } else if (mo < a.M) {
+    for (int turn = 0; turn < TURNS; ++turn) {
+      const int tile = turn * kShareWaves + wave, i = tile / TM, j = tile % TM;
+      const int col = n0 + 16 * i + 4 * g;
+      const int64_t row = m0 + 16 * j + r;
+      float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (nt + i < a.N) {
-        if (a.dtype == SVDC_F32)
-          static_cast<float*>(a.Out)[mo * a.ldo + nt + i] = v[i];
-        else
-          static_cast<bf16_t*>(a.Out)[mo * a.ldo + nt + i] = (bf16_t)v[i];
+      for (int w = 0; w < 8; ++w) top = fmaxf(top, tops[16 * j + r][w]);
+      const int byte = scale_byte(top);
+      const float inv = inverse_scale(byte);
+      if (row < a.M) {
+        *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.Out) + row * q8_row_bytes(a.N) + col) =
+            pack_e4m3(v[turn][0] * inv, v[turn][1] * inv, v[turn][2] * inv, v[turn][3] * inv);
+        uint8_t* os = a.Os + row * q8_scale_row_bytes(a.N);
+        if (i == 0 && g == 0) os[column_tile] = (uint8_t)byte;
+        if (i == 1 && g == 0 && column_tile == column_tiles - 1)
+          for (int s = column_tiles; s < q8_scale_row_bytes(a.N); ++s) os[s] = 127;
       }
+    }
   }
+}
+
+template <int TM, int TN, bool EXACT, bool GATED, bool EIGHT>
+__global__ __launch_bounds__(kShareWaves* kWave) void matmul8_shared_kernel(MatmulArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__          // buffer descriptors mean nothing to the host's pass
+  shared_sums<TM, TN, EXACT, GATED, EIGHT>(a);
+#endif
+}
+
+// The sums of `splits` parts of the columns of A and W, [splits][M][wide] float32, to Out: 16 lanes a block of 128 columns of a row.
+__global__ __launch_bounds__(256) void matmul8_finish_kernel(MatmulArgs a) {
+  const bool gated = a.act == SVDC_ACT_SWIGLU;
+  const int wide = gated ? 2 * a.N : a.N, out_blocks = q8_blocks(a.N);
+  const int64_t units = a.M * out_blocks;
+  for (int64_t unit = (int64_t)blockIdx.x * 16 + threadIdx.x / 16; unit < (units + 3) / 4 * 4; unit += (int64_t)gridDim.x * 16) {
+    const int64_t row = min(unit / out_blocks, a.M - 1);
+    const int block = (int)(unit % out_blocks), col = block * kScaleBlock + threadIdx.x % 16 * 8;
+    const float* from = a.partial + row * wide + col;
+    float v[8];
+    const int n = unit < units ? a.N - col : 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float z = 0.f, u = 0.f;
+      for (int s = 0; s < a.splits; ++s) {
+        if (e < n) z += from[(int64_t)s * a.M * wide + e];
+        if (gated && e < n) u += from[(int64_t)s * a.M * wide + a.N + e];
+      }
+      v[e] = finished(a, col + e, z, u);
+    }
+    if (a.dtype == SVDC_E4M3) {
+      float top = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+      const int byte = scale_byte(row16_max(top));
+      const float inv = inverse_scale(byte);
+      if (unit < units) {
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.Out) + row * q8_row_bytes(a.N) + col) =
+            uint2{pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv), pack_e4m3(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
+        uint8_t* os = a.Os + row * q8_scale_row_bytes(a.N);
+        if (threadIdx.x % 16 == 0) {
+          os[block] = (uint8_t)byte;
+          if (block == out_blocks - 1)
+            for (int s = out_blocks; s < q8_scale_row_bytes(a.N); ++s) os[s] = 127;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) {
+          if (a.dtype == SVDC_F32)
+            static_cast<float*>(a.Out)[row * a.ldo + col + e] = v[e];
+          else
+            static_cast<bf16_t*>(a.Out)[row * a.ldo + col + e] = (bf16_t)v[e];
+        }
+    }
   }
 }
 
@@ -147,7 +295,6 @@ __global__ __launch_bounds__(512) void matmul8_kernel(MatmulArgs a) {
 // 16 x 16 x 128, half the operand words).  Two stages of 128 columns of both operands lie in LDS, written by direct loads one block ahead; a wave's operands
 // lie in two register sets, one read from LDS while the other is multiplied.  Rows of 128 bytes are eight 16-byte slots; slot s of row r holds columns
 // 16 (s ^ swizzle(r)): eight consecutive rows and the rows of one parity of sixteen have different slots of a column, so that reads meet no bank twice.
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }   // a value that all lanes hold, as a scalar
 __device__ __forceinline__ int swizzle(int row) { return (row & 7) ^ (row >> 3 & 1); }
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -275,6 +422,13 @@ __device__ __forceinline__ void store_tile(const MatmulArgs& a, Acc& c, int64_t 
   }
 }
 
+// Values loaded before the last wait for LDS' loads: known here to be there, so that no use of them waits for loads issued since
+template <int N>
+__device__ __forceinline__ void arrived(int (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
+}
+
 template <int TM, int TN>
 struct TileStage {
   __align__(1024) uint8_t b[64 * (TM + TN) * 128];
@@ -293,7 +447,11 @@ __device__ __forceinline__ void tile_at(int id, int row_tiles, int column_tiles,
 template <int TM, int TN, int ACT, int ES>
 __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
   constexpr bool EXACT = ES == 4, GATED = ACT == SVDC_ACT_SWIGLU;
-  constexpr int BM = 64 * TM, BN = 64 * TN, LOADS = (BM + BN) / 32, READ = TM * TN > 4 ? TN + TM + 1 : TN * TM - 1;
+  constexpr int BM = 64 * TM, BN = 64 * TN, LOADS = (BM + BN) / 32;
+  // A half block is SLOTS instructions long.  Once the second half has been read, at READ, its block's stage is loaded anew: FIRST loads in the rest of the first
+  // half, the others in the first LATE slots of the second.  A load takes 16 cycles of its unit, four waves' 64: more than one a slot of 64 cycles
+  // hold up the wave, and with it its products (16 loads in 7 slots: 2475 TFLOP/s at 8192 x 8192 x 8192, so dealt out 2617).
+  constexpr int SLOTS = TM * TN, READ = SLOTS == 16 ? 10 : SLOTS - 1, FIRST = SLOTS == 16 ? 6 : LOADS / 2, LATE = SLOTS == 16 ? 10 : SLOTS;
   __shared__ TileStage<TM, TN> stage0;
   __shared__ TileStage<TM, TN> stage1;
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -338,11 +496,6 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
   const int f = swizzle(r);
   const int slot[4] = {((2 * h) ^ f) * 16, ((2 * h + 1) ^ f) * 16, ((4 + 2 * h) ^ f) * 16, ((5 + 2 * h) ^ f) * 16};
   const int a_base = (wm * 32 * TM + r) * 128, w_base = (BM + wn * 32 * TN + r) * 128;
-  const auto operand = [&](const uint8_t* stage, int t, int half) {       // t < TN: of W, else of A
-    const uint8_t* row = stage + (t < TN ? w_base + t * 4096 : a_base + (t - TN) * 4096);
-    const u32x4 lo = *reinterpret_cast<const u32x4*>(row + slot[2 * half]), hi = *reinterpret_cast<const u32x4*>(row + slot[2 * half + 1]);
-    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-  };
 
   // scales of four blocks at a time, those of the current block in the lowest byte
   const auto As = rows_of(a.As + m0 * ss, uniform((int)min<int64_t>(BM, a.M - m0) * ss)), Ws = rows_of(a.Ws, uniform(q8_blocks(gated ? 2 * a.N : a.N) * ss));
@@ -357,6 +510,12 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
     for (int t = 0; t < TN + TM; ++t) s[t] = __builtin_amdgcn_raw_buffer_load_b32(t < TN ? Ws : As, scale_row[t], b, 0);
   };
 
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j) load(j, 0, stage0.b, A1, W1, U1);
+  if (blocks > 1) {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) load(j, 1, stage1.b, A1, W1, U1);
+  }
   // the sums start at the bias: bounds-checked loads, zero beyond the last column and without one
   const uint8_t* const bias_bytes = reinterpret_cast<const uint8_t*>(a.bias);
   const auto bias_z = rows_of(bias_bytes, uniform(a.bias ? a.N * 4 : 0)),
@@ -376,17 +535,21 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
   i32x8 x[2][TN + TM];
 
   load_scales(0, sc);
-  load_scales(min(4, ss - 4), next_sc);
+  // Piece p of 2 (TN + TM) of the operands of a half block, in the order in which they are multiplied
+  constexpr int PIECES = 2 * (TN + TM);
+  const auto operand_of = [](int p) { return p / 2 == 0 ? 0 : p / 2 <= TM ? TN + p / 2 - 1 : p / 2 - TM; };
+  const auto read = [&](i32x8* y, const uint8_t* stage, int p, int half) {
+    const int t = operand_of(p);
+    const uint8_t* row = stage + (t < TN ? w_base + t * 4096 : a_base + (t - TN) * 4096);
+    const u32x4 v = *reinterpret_cast<const u32x4*>(row + slot[2 * half + p % 2]);
 #pragma unroll
-  for (int j = 0; j < LOADS; ++j) load(j, 0, stage0.b, A1, W1, U1);
-  if (blocks > 1) {
-#pragma unroll
-    for (int j = 0; j < LOADS; ++j) load(j, 1, stage1.b, A1, W1, U1);
-  }
+    for (int e = 0; e < 4; ++e) y[t][4 * (p % 2) + e] = (int)v[e];
+  };
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  arrived(sc);
   __syncthreads();
 #pragma unroll
-  for (int t = 0; t < TN + TM; ++t) x[0][t] = operand(stage0.b, t, 0);
+  for (int p = 0; p < PIECES; ++p) read(x[0], stage0.b, p, 0);
 
   const auto multiply = [&](const i32x8* y, auto&& between) {
 #pragma unroll
@@ -399,38 +562,52 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
         __builtin_amdgcn_sched_barrier(0);
       }
   };
-  // Block b lies in `now` with its first half in x[0].  Once all waves have read its second half, block b + 2 is loaded there (beyond the last one the
-  // loads are out of bounds and fetch nothing); it has a block and a half's time to arrive.
+  // Block b lies in `now` with its first half in x[0].  Once all waves have read its second half, block b + 2 is loaded there; beyond the last one the
+  // loads are out of bounds and fetch nothing.
   const auto block = [&](int b, uint8_t* now, uint8_t* then) {
     const int more = b + 2 < blocks ? -1 : 0;
     const auto A2 = rows_of(a.A + m0 * Kp, a_bytes & more), W2 = rows_of(a.W + n0 * Kp, w_bytes & more), U2 = rows_of(a.W + u_first * Kp, w_bytes & more);
     multiply(x[0], [&](int t) {
-      if (t < TN + TM) x[1][t] = operand(now, t, 1);
+      if (2 * t < PIECES) {
+        read(x[1], now, 2 * t, 1);
+        read(x[1], now, 2 * t + 1, 1);
+      }
       if (t == READ) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       if (t >= READ) {
 #pragma unroll
-        for (int j = (t - READ) * LOADS / (TN * TM - READ); j < (t - READ + 1) * LOADS / (TN * TM - READ); ++j) load(j, b + 2, now, A2, W2, U2);
+        for (int j = (t - READ) * FIRST / (SLOTS - READ); j < (t - READ + 1) * FIRST / (SLOTS - READ); ++j) load(j, b + 2, now, A2, W2, U2);
       }
     });
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(FIRST) : "memory");
     multiply(x[1], [&](int t) {
-      if (t < TN + TM) x[0][t] = operand(then, t, 0);
+#pragma unroll
+      for (int p = t * PIECES / SLOTS; p < (t + 1) * PIECES / SLOTS; ++p) read(x[0], then, p, 0);
+      if (t < LATE) {
+#pragma unroll
+        for (int j = FIRST + t * (LOADS - FIRST) / LATE; j < FIRST + (t + 1) * (LOADS - FIRST) / LATE; ++j) load(j, b + 2, now, A2, W2, U2);
+      }
     });
-    if ((b & 3) == 3) {
 #pragma unroll
-      for (int t = 0; t < TN + TM; ++t) sc[t] = next_sc[t];
-      load_scales(min(b + 5, ss - 4), next_sc);
-    } else {
-#pragma unroll
-      for (int t = 0; t < TN + TM; ++t) sc[t] = (int)((uint32_t)sc[t] >> 8);
-    }
+    for (int t = 0; t < TN + TM; ++t) sc[t] = (int)((uint32_t)sc[t] >> 8);
   };
   int b = 0;
-  for (; b + 1 < blocks; b += 2) {
+  for (; b + 3 < blocks; b += 4) {
+    load_scales(min(b + 4, ss - 4), next_sc);
     block(b, stage0.b, stage1.b);
     block(b + 1, stage1.b, stage0.b);
+    block(b + 2, stage0.b, stage1.b);
+    block(b + 3, stage1.b, stage0.b);
+    arrived(next_sc);
+#pragma unroll
+    for (int t = 0; t < TN + TM; ++t) sc[t] = next_sc[t];
   }
-  if (b < blocks) block(b, stage0.b, stage1.b);
+  if (b < blocks) {
+    block(b, stage0.b, stage1.b);
+    if (b + 1 < blocks) {
+      block(b + 1, stage1.b, stage0.b);
+      if (b + 2 < blocks) block(b + 2, stage0.b, stage1.b);
+    }
+  }
   asm volatile("s_waitcnt lgkmcnt(0) vmcnt(0)\n\ts_barrier" ::: "memory");
   const bool edge = n0 + columns > a.N || column_tile == column_tiles - 1;
   store_tile<TM, TN, ACT, ES>(a, c, m0, n0, edge, wm, wn, lane, stage0.b, reinterpret_cast<float*>(stage1.b));
@@ -444,11 +621,20 @@ __global__ __launch_bounds__(256) void matmul8_tile_kernel(MatmulArgs a) {
 #endif
 }
 
-}  // namespace
+// ---- which of them ---------------------------------------------------------------------------------------------------
 
-size_t matmul8_workspace_bytes(const svdc_matmul8&) { return 0; }
+// How a product is made: `rows` 16, 32 or 64: workgroups of that many rows by 64 columns (128 for results in 8 bits) whose waves share the blocks,
+// `splits` of them for a tile; 128, 256: tiles of that size through LDS.
+struct MatmulPlan {
+  int rows, splits;
+};
 
-namespace {
+int wide_of(const svdc_matmul8& p) { return p.act == SVDC_ACT_SWIGLU ? 2 * p.N : p.N; }
+
+MatmulPlan matmul8_plan(const svdc_matmul8& p) {
+  if (p.M >= 64) return {p.dtype == SVDC_F32 ? 128 : 256, 1};
+  return {p.M > 16 ? 32 : 16, 1};
+}
 
 template <int TM, int TN, int ACT, int ES>
 void launch_tiles(const MatmulArgs& a, hipStream_t st) {
@@ -457,38 +643,78 @@ void launch_tiles(const MatmulArgs& a, hipStream_t st) {
   matmul8_tile_kernel<TM, TN, ACT, ES><<<(unsigned)tiles, 256, 0, st>>>(a);
 }
 
-template <int TM, int TN, int ES>
+// results in 8 bits need a whole block of columns in a tile of gated rows too
+template <int T, int ES>
 void launch_tiles(const MatmulArgs& a, hipStream_t st) {
   if (a.act == SVDC_ACT_SWIGLU)
-    launch_tiles<TM, TN, SVDC_ACT_SWIGLU, ES>(a, st);
+    launch_tiles<T, T == 2 && ES == 1 ? 4 : T, SVDC_ACT_SWIGLU, ES>(a, st);
   else if (a.act == SVDC_ACT_GELU)
-    launch_tiles<TM, TN, SVDC_ACT_GELU, ES>(a, st);
+    launch_tiles<T, T, SVDC_ACT_GELU, ES>(a, st);
   else
-    launch_tiles<TM, TN, SVDC_ACT_NONE, ES>(a, st);
+    launch_tiles<T, T, SVDC_ACT_NONE, ES>(a, st);
+}
+
+template <int TM, int TN, bool EXACT, bool GATED, bool EIGHT>
+void launch_shared(const MatmulArgs& a, hipStream_t st) {
+  const int64_t tiles = (a.M + 16 * TM - 1) / (16 * TM) * ((a.N + 16 * TN - 1) / (16 * TN));
+  matmul8_shared_kernel<TM, TN, EXACT, GATED, EIGHT><<<dim3((unsigned)tiles, a.splits), kShareWaves * kWave, 0, st>>>(a);
+}
+
+template <bool EXACT, bool GATED>
+void launch_shared(const MatmulArgs& a, int rows, hipStream_t st) {
+  if (rows == 16)
+    launch_shared<1, 4, EXACT, GATED, false>(a, st);
+  else if (rows == 32)
+    launch_shared<2, 4, EXACT, GATED, false>(a, st);
+  else
+    launch_shared<4, GATED ? 2 : 4, EXACT, GATED, false>(a, st);
+}
+
+void launch_shared(const MatmulArgs& a, int rows, hipStream_t st) {
+  const bool gated = a.act == SVDC_ACT_SWIGLU;
+  if (a.dtype == SVDC_F32)
+    gated ? launch_shared<true, true>(a, rows, st) : launch_shared<true, false>(a, rows, st);
+  else if (a.dtype == SVDC_BF16 || a.partial)
+    gated ? launch_shared<false, true>(a, rows, st) : launch_shared<false, false>(a, rows, st);
+  else if (gated)
+    launch_shared<1, 8, false, true, true>(a, st);
+  else
+    rows == 16 ? launch_shared<1, 8, false, false, true>(a, st) : launch_shared<2, 8, false, false, true>(a, st);
+}
+
+int32_t launch_planned(const svdc_matmul8& p, const MatmulPlan& plan, MatmulArgs a, void* workspace, hipStream_t st) {
+  a.splits = plan.splits;
+  if (plan.rows == 256) {
+    p.dtype == SVDC_BF16 ? launch_tiles<4, 2>(a, st) : launch_tiles<4, 1>(a, st);
+  } else if (plan.rows == 128) {
+    p.dtype == SVDC_F32 ? launch_tiles<2, 4>(a, st) : p.dtype == SVDC_BF16 ? launch_tiles<2, 2>(a, st) : launch_tiles<2, 1>(a, st);
+  } else if (plan.splits == 1) {
+    launch_shared(a, plan.rows, st);
+  } else {
+    a.partial = static_cast<float*>(workspace);
+    MatmulArgs part = a;                       // plain sums of all of W's rows
+    part.N = wide_of(p);
+    part.act = SVDC_ACT_NONE;
+    launch_shared(part, plan.rows, st);
+    if (hipGetLastError() != hipSuccess) return SVDC_E_HIP;
+    const int64_t groups = (p.M * q8_blocks(p.N) + 15) / 16;
+    matmul8_finish_kernel<<<(unsigned)std::min<int64_t>(groups, 1 << 20), 256, 0, st>>>(a);
+  }
+  return launch_status();
 }
 
 }  // namespace
 
+size_t matmul8_workspace_bytes(const svdc_matmul8& p) {
+  const MatmulPlan plan = matmul8_plan(p);
+  return plan.splits == 1 ? 0 : (size_t)plan.splits * p.M * wide_of(p) * sizeof(float);
+}
+
 int32_t launch_matmul8(const svdc_matmul8& p, const void* A, const void* As, const void* W, const void* Ws, const float* bias, void* Out, void* Os,
-                       void*, hipStream_t st) {
+                       void* workspace, hipStream_t st) {
   const MatmulArgs a{static_cast<const uint8_t*>(A), static_cast<const uint8_t*>(As), static_cast<const uint8_t*>(W), static_cast<const uint8_t*>(Ws),
-                     bias, Out, static_cast<uint8_t*>(Os), p.M, p.ldo, p.N, p.K, p.dtype, p.act};
-  if (p.M >= 64) {
-    if (p.dtype == SVDC_F32)
-      launch_tiles<2, 2, 4>(a, st);
-    else if (p.dtype == SVDC_BF16)
-      launch_tiles<4, 4, 2>(a, st);
-    else
-      launch_tiles<4, 4, 1>(a, st);
-    return launch_status();
-  }
-  const int64_t tiles = (p.M + 15) / 16 * q8_blocks(p.N);
-  const unsigned grid = (unsigned)std::min<int64_t>(tiles, 1 << 20);
-  if (p.dtype == SVDC_F32)
-    matmul8_kernel<true><<<grid, 512, 0, st>>>(a);
-  else
-    matmul8_kernel<false><<<grid, 512, 0, st>>>(a);
-  return launch_status();
+                     bias, Out, static_cast<uint8_t*>(Os), nullptr, p.M, p.ldo, p.N, p.K, p.dtype, p.act, 1};
+  return launch_planned(p, matmul8_plan(p), a, workspace, st);
 }
 
 }  // namespace svdc
