@@ -26,7 +26,6 @@ struct MatmulArgs {
   const float* bias;
   void* Out;
   uint8_t* Os;
-  float* partial;      // sums of parts of the columns of A and W, or nullptr
   int64_t M, ldo;
   int N, K, dtype, act, splits;
 };
@@ -80,13 +79,13 @@ __device__ __forceinline__ float finished(const MatmulArgs& a, int col, float z,
 //
 // Where there are not enough large tiles to occupy the card, a workgroup makes 16 TM rows by 16 TN columns and its eight waves share the blocks of columns of
 // A and W: wave w takes blocks w, w + 8, ... straight from memory into registers (nothing is used twice within a wave), and the eight sums are added through
-// LDS, always in the same order.  What it costs is the weights' bytes for few rows, and the operands' way out of L2 for many.
+// LDS, always in the same order.
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }   // a value that all lanes hold, as a scalar
 
 // a buffer for bounds-checked accesses: loads beyond its end give zero
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t bounded(const void* p, int64_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, uniform((int)bytes), 0x00027000);
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t bounded(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
 }
 
 constexpr int kShareWaves = 8;
@@ -95,7 +94,8 @@ constexpr int kShareWaves = 8;
 template <int TM, int TN, bool EXACT, bool GATED, bool EIGHT>
 __device__ __forceinline__ void shared_sums(const MatmulArgs& a) {
   constexpr int NW = GATED ? 2 * TN : TN, COLUMNS = 16 * TN, ROWS = 16 * TM;
-  constexpr bool AHEAD = (TM + NW) * 16 + TM * NW * 4 + (EXACT ? 48 : 0) <= 200;   // registers for the operands of the next block too
+  constexpr int FREE = 190 - TM * NW * 4 - (EXACT ? 40 : 0), EACH = (TM + NW) * 9;   // registers: for operands, and those of a block
+  constexpr int DEPTH = FREE / EACH < 1 ? 1 : FREE / EACH > 3 ? 3 : FREE / EACH;     // blocks in flight
   __shared__ f32x4 sums[kShareWaves][NW * TM][kWave];
   __shared__ float tops[TM * 16][8];
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
@@ -106,57 +106,83 @@ __device__ __forceinline__ void shared_sums(const MatmulArgs& a) {
   const int64_t m0 = (int64_t)row_tile * ROWS;
   const int n0 = column_tile * COLUMNS, rows = (int)min<int64_t>(ROWS, a.M - m0), columns = min(COLUMNS, a.N - n0);
 
-  const auto A = bounded(a.A + m0 * Kp, rows * Kp), W = bounded(a.W + n0 * Kp, columns * Kp),
-             U = bounded(a.W + ((GATED ? (int64_t)a.N : 0) + n0) * Kp, columns * Kp);
-  const auto As = bounded(a.As + m0 * ss, rows * ss), Ws = bounded(a.Ws, (int64_t)q8_blocks(GATED ? 2 * a.N : a.N) * ss);
+  const int a_bytes = uniform((int)(rows * Kp)), w_bytes = uniform((int)(columns * Kp));
+  const int as_bytes = uniform(rows * ss), ws_bytes = uniform((int)((int64_t)q8_blocks(GATED ? 2 * a.N : a.N) * ss));
   // a lane's 32 bytes of a row are 16 from each half of a block, so that a load takes 64 bytes in a row
-  uint32_t at[TM + NW], scale_at[TM + NW];
+  uint32_t at[TM + NW];
 #pragma unroll
-  for (int t = 0; t < TM + NW; ++t) {
-    const int i = (t < TM ? t : (t - TM) % TN) * 16 + r, up = t >= TM + TN ? a.N : 0;
-    at[t] = (uint32_t)(i * Kp + 16 * g);
-    scale_at[t] = (uint32_t)(t < TM ? i * ss : (min(n0 + i, a.N - 1) + up) / kScaleBlock * ss);
-  }
+  for (int t = 0; t < TM + NW; ++t) at[t] = (uint32_t)(((t < TM ? t : (t - TM) % TN) * 16 + r) * Kp + 16 * g);
+  // scales: of TM tiles of A; one for all columns, as they lie in one block of 128; of what the gates gate, whose blocks begin anywhere, each row's own
+  constexpr int SCALES = TM + 1 + (GATED ? TN : 0);
+  uint32_t scale_at[SCALES];
+#pragma unroll
+  for (int t = 0; t < SCALES; ++t)
+    scale_at[t] = (uint32_t)(t < TM    ? (t * 16 + r) * ss
+                             : t == TM ? n0 / kScaleBlock * ss
+                                       : (a.N + min(n0 + (t - TM - 1) * 16 + r, a.N - 1)) / kScaleBlock * ss);
   struct Operands {
     i32x8 x[TM + NW];
-    int s[TM + NW];
+    int s[SCALES];
   };
   const auto load = [&](int b, Operands& o) {
+    const int any = b < blocks ? -1 : 0;
+    const auto A = bounded(a.A + m0 * Kp, a_bytes & any), W = bounded(a.W + n0 * Kp, w_bytes & any),
+               U = bounded(a.W + ((GATED ? (int64_t)a.N : 0) + n0) * Kp, w_bytes & any);
+    const auto As = bounded(a.As + m0 * ss, as_bytes & any), Ws = bounded(a.Ws, ws_bytes & any);
+#pragma unroll
+    for (int t = 0; t < SCALES; ++t) o.s[t] = __builtin_amdgcn_raw_buffer_load_b32(t < TM ? As : Ws, scale_at[t], uniform(b & ~3), 0);
 #pragma unroll
     for (int t = 0; t < TM + NW; ++t) {
       const auto from = t < TM ? A : t < TM + TN ? W : U;
       const auto lo = __builtin_amdgcn_raw_buffer_load_b128(from, at[t], uniform(b * 128), 0),
                  hi = __builtin_amdgcn_raw_buffer_load_b128(from, at[t], uniform(b * 128 + 64), 0);
       o.x[t] = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-      o.s[t] = __builtin_amdgcn_raw_buffer_load_b8(t < TM ? As : Ws, scale_at[t], uniform(b), 0);
     }
   };
   f32x4 c[NW][TM] = {};
-  const auto multiply = [&](const Operands& o) {
+  const auto multiply = [&](int b, const Operands& o) {
+    int s[SCALES];                         // the block's byte, lowest
+#pragma unroll
+    for (int t = 0; t < SCALES; ++t) {
+      s[t] = o.s[t];
+      asm volatile("" : "+v"(s[t]));       // not before this block's turn, or it would wait for the loads of all of them
+      s[t] = (int)((uint32_t)s[t] >> (b & 3) * 8);
+      if (EXACT) s[t] &= 255;
+    }
 #pragma unroll
     for (int i = 0; i < NW; ++i)
 #pragma unroll
-      for (int j = 0; j < TM; ++j) c[i][j] = product<EXACT>(o.x[TM + i], o.x[j], c[i][j], o.s[TM + i], o.s[j]);
+      for (int j = 0; j < TM; ++j) c[i][j] = product<EXACT>(o.x[TM + i], o.x[j], c[i][j], s[i < TN ? TM : TM + 1 + i - TN], s[j]);
   };
-  const int each = (blocks + a.splits - 1) / a.splits, first = uniform(blockIdx.y * each), last = uniform(min(blocks, first + each));
-  if (AHEAD) {
-    Operands o[2];
-    int b = first + wave;
-    if (b < last) load(b, o[0]);
-    for (; b < last; b += 2 * kShareWaves) {
-      if (b + kShareWaves < last) load(b + kShareWaves, o[1]);
-      multiply(o[0]);
-      if (b + kShareWaves < last) {
-        if (b + 2 * kShareWaves < last) load(b + 2 * kShareWaves, o[0]);
-        multiply(o[1]);
+  Operands o[DEPTH];
+  int b = wave;
+  if (b + DEPTH * kShareWaves < blocks) {
+    // Loads and products of a round are made whether its blocks are there or not (behind the last one the buffers have no bytes and give zeros): behind
+    // conditions, the compiler would wait for each block's loads before the next block's were of any use.
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      load(b + d * kShareWaves, o[d]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    for (; b + DEPTH * kShareWaves < blocks; b += DEPTH * kShareWaves) {
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        multiply(b + d * kShareWaves, o[d]);
+        __builtin_amdgcn_sched_barrier(0);
+        load(b + (d + DEPTH) * kShareWaves, o[d]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) multiply(b + d * kShareWaves, o[d]);
   } else {
-    for (int b = first + wave; b < last; b += kShareWaves) {
-      Operands o;
-      load(b, o);
-      multiply(o);
-    }
+    // all at once, and no loads for nothing: they cost as much as others
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+      if (b + d * kShareWaves < blocks) load(b + d * kShareWaves, o[d]);
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+      if (b + d * kShareWaves < blocks) multiply(b + d * kShareWaves, o[d]);
   }
 #pragma unroll
   for (int i = 0; i < NW; ++i)
@@ -179,15 +205,6 @@ __device__ __forceinline__ void shared_sums(const MatmulArgs& a) {
     }
     const int col = n0 + 16 * i + 4 * g;
     const int64_t row = m0 + 16 * j + r;
-    if (a.partial) {
-      if (row < a.M) {
-        float* to = a.partial + ((int64_t)blockIdx.y * a.M + row) * a.N + col;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (col + e < a.N) to[e] = z[e];
-      }
-      continue;
-    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[turn][e] = finished(a, col + e, z[e], GATED ? u[e] : 0.f);
     if (EIGHT) {
@@ -238,55 +255,6 @@ __global__ __launch_bounds__(kShareWaves* kWave) void matmul8_shared_kernel(Matm
 #ifdef __HIP_DEVICE_COMPILE__          // buffer descriptors mean nothing to the host's pass
   shared_sums<TM, TN, EXACT, GATED, EIGHT>(a);
 #endif
-}
-
-// The sums of `splits` parts of the columns of A and W, [splits][M][wide] float32, to Out: 16 lanes a block of 128 columns of a row.
-__global__ __launch_bounds__(256) void matmul8_finish_kernel(MatmulArgs a) {
-  const bool gated = a.act == SVDC_ACT_SWIGLU;
-  const int wide = gated ? 2 * a.N : a.N, out_blocks = q8_blocks(a.N);
-  const int64_t units = a.M * out_blocks;
-  for (int64_t unit = (int64_t)blockIdx.x * 16 + threadIdx.x / 16; unit < (units + 3) / 4 * 4; unit += (int64_t)gridDim.x * 16) {
-    const int64_t row = min(unit / out_blocks, a.M - 1);
-    const int block = (int)(unit % out_blocks), col = block * kScaleBlock + threadIdx.x % 16 * 8;
-    const float* from = a.partial + row * wide + col;
-    float v[8];
-    const int n = unit < units ? a.N - col : 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float z = 0.f, u = 0.f;
-      for (int s = 0; s < a.splits; ++s) {
-        if (e < n) z += from[(int64_t)s * a.M * wide + e];
-        if (gated && e < n) u += from[(int64_t)s * a.M * wide + a.N + e];
-      }
-      v[e] = finished(a, col + e, z, u);
-    }
-    if (a.dtype == SVDC_E4M3) {
-      float top = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
-      const int byte = scale_byte(row16_max(top));
-      const float inv = inverse_scale(byte);
-      if (unit < units) {
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.Out) + row * q8_row_bytes(a.N) + col) =
-            uint2{pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv), pack_e4m3(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
-        uint8_t* os = a.Os + row * q8_scale_row_bytes(a.N);
-        if (threadIdx.x % 16 == 0) {
-          os[block] = (uint8_t)byte;
-          if (block == out_blocks - 1)
-            for (int s = out_blocks; s < q8_scale_row_bytes(a.N); ++s) os[s] = 127;
-        }
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < n) {
-          if (a.dtype == SVDC_F32)
-            static_cast<float*>(a.Out)[row * a.ldo + col + e] = v[e];
-          else
-            static_cast<bf16_t*>(a.Out)[row * a.ldo + col + e] = (bf16_t)v[e];
-        }
-    }
-  }
 }
 
 // ---- tiles ----------------------------------------------------------------------------------------------------------
@@ -444,9 +412,9 @@ __device__ __forceinline__ void tile_at(int id, int row_tiles, int column_tiles,
   column = uniform(at / high);
 }
 
-template <int TM, int TN, int ACT, int ES>
-__device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
-  constexpr bool EXACT = ES == 4, GATED = ACT == SVDC_ACT_SWIGLU;
+template <int TM, int TN, int ACT, int ES, bool EXACT>
+__device__ __forceinline__ void tile_of_product(MatmulArgs a) {
+  constexpr bool GATED = ACT == SVDC_ACT_SWIGLU;
   constexpr int BM = 64 * TM, BN = 64 * TN, LOADS = (BM + BN) / 32;
   // A half block is SLOTS instructions long.  Once the second half has been read, at READ, its block's stage is loaded anew: FIRST loads in the rest of the first
   // half, the others in the first LATE slots of the second.  A load takes 16 cycles of its unit, four waves' 64: more than one a slot of 64 cycles
@@ -458,7 +426,15 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
   const int wm = wave & 1, wn = wave >> 1;
   constexpr bool gated = GATED;
   const int64_t Kp = q8_row_bytes(a.K);
-  const int blocks = uniform(q8_blocks(a.K)), ss = uniform(q8_scale_row_bytes(a.K));
+  const int ss = uniform(q8_scale_row_bytes(a.K));
+  // this part's blocks of columns of A and W: a multiple of four each, as scales are read four at a time
+  const int all = q8_blocks(a.K), each = ((all + a.splits - 1) / a.splits + 3) / 4 * 4, skip = uniform(a.splits == 1 ? 0 : blockIdx.y * each);
+  const int blocks = uniform(a.splits == 1 ? all : min(each, all - skip));
+  a.A += (int64_t)skip * 128;
+  a.W += (int64_t)skip * 128;
+  a.As += skip;
+  a.Ws += skip;
+  if (ES == 4) a.Out = static_cast<float*>(a.Out) + blockIdx.y * a.M * a.ldo;
   const int columns = gated ? BN / 2 : BN;                  // of Out
   const int column_tiles = (a.N + columns - 1) / columns;
   const int row_tiles = (int)((a.M + BM - 1) / BM);
@@ -478,7 +454,7 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
 
   // This wave's pieces of 8 rows of a stage: bounds-checked loads from A, the gates and what they multiply, each from the tile's first row on
   const auto rows_of = [](const uint8_t* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, bytes, 0x00027000); };
-  const int a_bytes = uniform((int)(min<int64_t>(BM, a.M - m0) * Kp)), w_bytes = uniform((int)(min(columns, a.N - n0) * Kp));
+  const int a_bytes = uniform((int)(min<int64_t>(BM, a.M - m0) * Kp - skip * 128)), w_bytes = uniform((int)(min(columns, a.N - n0) * Kp - skip * 128));
   const int64_t u_first = (gated ? (int64_t)a.N : 0) + n0;
   const auto A1 = rows_of(a.A + m0 * Kp, a_bytes), W1 = rows_of(a.W + n0 * Kp, w_bytes), U1 = rows_of(a.W + u_first * Kp, w_bytes);
   const auto is_up = [](int j) { return GATED && (j * 32 - BM) % (32 * TN) >= 16 * TN; };
@@ -498,7 +474,7 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
   const int a_base = (wm * 32 * TM + r) * 128, w_base = (BM + wn * 32 * TN + r) * 128;
 
   // scales of four blocks at a time, those of the current block in the lowest byte
-  const auto As = rows_of(a.As + m0 * ss, uniform((int)min<int64_t>(BM, a.M - m0) * ss)), Ws = rows_of(a.Ws, uniform(q8_blocks(gated ? 2 * a.N : a.N) * ss));
+  const auto As = rows_of(a.As + m0 * ss, uniform((int)min<int64_t>(BM, a.M - m0) * ss - skip)), Ws = rows_of(a.Ws, uniform(q8_blocks(gated ? 2 * a.N : a.N) * ss - skip));
   uint32_t scale_row[TN + TM];
 #pragma unroll
   for (int t = 0; t < TN; ++t) scale_row[t] = (uint32_t)(w_row(wn * 32 * TN + t * 32 + r) / kScaleBlock * ss);
@@ -592,7 +568,7 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
   };
   int b = 0;
   for (; b + 3 < blocks; b += 4) {
-    load_scales(min(b + 4, ss - 4), next_sc);
+    load_scales(min(b + 4, ss - skip - 4), next_sc);
     block(b, stage0.b, stage1.b);
     block(b + 1, stage1.b, stage0.b);
     block(b + 2, stage0.b, stage1.b);
@@ -613,92 +589,186 @@ __device__ __forceinline__ void tile_of_product(const MatmulArgs& a) {
   store_tile<TM, TN, ACT, ES>(a, c, m0, n0, edge, wm, wn, lane, stage0.b, reinterpret_cast<float*>(stage1.b));
 }
 
-// ACT: svdc_act;  ES: bytes of an element of Out
-template <int TM, int TN, int ACT, int ES>
+// ACT: svdc_act;  ES: bytes of an element of Out;  EXACT: float32 sums.  Part blockIdx.y of a.splits of the columns of A and W
+template <int TM, int TN, int ACT, int ES, bool EXACT>
 __global__ __launch_bounds__(256) void matmul8_tile_kernel(MatmulArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__          // buffer descriptors and accumulation registers mean nothing to the host's pass
-  tile_of_product<TM, TN, ACT, ES>(a);
+  tile_of_product<TM, TN, ACT, ES, EXACT>(a);
 #endif
+}
+
+// The sums of `splits` parts of the columns of A and W, [splits][M][wide] float32, to Out: 16 lanes a block of 128 columns of a row, parts in order.
+__global__ __launch_bounds__(256) void matmul8_finish_kernel(MatmulArgs a, const float* parts) {
+  const bool gated = a.act == SVDC_ACT_SWIGLU;
+  const int wide = gated ? 2 * a.N : a.N, out_blocks = q8_blocks(a.N);
+  const int64_t units = a.M * out_blocks, part = a.M * wide;
+  const auto add8 = [&](const float* from, int n, float (&v)[8]) {
+    for (int s = 0; s < a.splits; ++s, from += part) {
+      if (n >= 8) {
+        const u32x4_any lo = reinterpret_cast<const u32x4_any*>(from)[0], hi = reinterpret_cast<const u32x4_any*>(from)[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += __uint_as_float(lo[e]), v[4 + e] += __uint_as_float(hi[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < n) v[e] += from[e];
+      }
+    }
+  };
+  // whole groups of four units, as the lanes of a wave work on the maxima together
+  for (int64_t unit = (int64_t)blockIdx.x * 16 + threadIdx.x / 16; unit < (units + 3) / 4 * 4; unit += (int64_t)gridDim.x * 16) {
+    const bool has = unit < units;
+    const int64_t row = has ? unit / out_blocks : 0;
+    const int block = has ? (int)(unit - row * out_blocks) : 0, col = block * kScaleBlock + threadIdx.x % 16 * 8, n = has ? a.N - col : 0;
+    float v[8] = {}, u[8] = {};
+    add8(parts + row * wide + col, n, v);
+    if (gated) add8(parts + row * wide + a.N + col, n, u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = finished(a, col + e, v[e], u[e]);
+    if (a.dtype == SVDC_E4M3) {
+      float top = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+      const int byte = scale_byte(row16_max(top));
+      const float inv = inverse_scale(byte);
+      if (!has) continue;
+      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.Out) + row * q8_row_bytes(a.N) + col) =
+          uint2{pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv), pack_e4m3(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
+      uint8_t* os = a.Os + row * q8_scale_row_bytes(a.N);
+      if (threadIdx.x % 16 == 0) {
+        os[block] = (uint8_t)byte;
+        if (block == out_blocks - 1)
+          for (int s = out_blocks; s < q8_scale_row_bytes(a.N); ++s) os[s] = 127;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) {
+          if (a.dtype == SVDC_F32)
+            static_cast<float*>(a.Out)[row * a.ldo + col + e] = v[e];
+          else
+            static_cast<bf16_t*>(a.Out)[row * a.ldo + col + e] = (bf16_t)v[e];
+        }
+    }
+  }
 }
 
 // ---- which of them ---------------------------------------------------------------------------------------------------
 
-// How a product is made: `rows` 16, 32 or 64: workgroups of that many rows by 64 columns (128 for results in 8 bits) whose waves share the blocks,
-// `splits` of them for a tile; 128, 256: tiles of that size through LDS.
+// How a product is made.  rows 16 or 32: workgroups of that many rows by `columns` (16, 32, 64, or 128 for results in 8 bits) whose waves share the blocks;
+// rows 128 or 256: tiles of that size through LDS, `splits` parts of the columns of A and W (of 128 only).
 struct MatmulPlan {
-  int rows, splits;
+  int rows, columns, splits;
 };
 
 int wide_of(const svdc_matmul8& p) { return p.act == SVDC_ACT_SWIGLU ? 2 * p.N : p.N; }
 
-MatmulPlan matmul8_plan(const svdc_matmul8& p) {
-  if (p.M >= 64) return {p.dtype == SVDC_F32 ? 128 : 256, 1};
-  return {p.M > 16 ? 32 : 16, 1};
+// parts of the columns of A and W of which none is empty: a tile takes a multiple of four blocks
+int parts_of(int blocks, int splits) {
+  const int each = ((blocks + splits - 1) / splits + 3) / 4 * 4;
+  return (blocks + each - 1) / each;
 }
 
-template <int TM, int TN, int ACT, int ES>
+MatmulPlan matmul8_plan(const svdc_matmul8& p) {
+  const bool gated = p.act == SVDC_ACT_SWIGLU, exact = p.dtype == SVDC_F32, eight = p.dtype == SVDC_E4M3;
+  const double units = num_compute_units();
+  const int blocks = q8_blocks(p.K);
+  const auto up = [](double x, double y) { return (double)(int64_t)((x + y - 1) / y); };
+  MatmulPlan best{};
+  double least = 1e300;
+  const auto consider = [&](MatmulPlan plan, double us) {
+    if (us < least) least = us, best = plan;
+  };
+  for (int rows = 16; rows <= 32; rows *= 2)
+    for (int columns = eight ? 128 : 16; columns <= (eight ? 128 : gated ? 32 : 64); columns *= 2) {
+      if (rows == 32 && ((eight && gated) || p.M <= 16)) continue;
+      const double tiles = up((double)p.M, rows) * up(p.N, columns);
+      const double loads = columns / 16 * (gated ? 2 : 1) + std::min(rows, (int)std::min<int64_t>(p.M, rows)) / 16.0;
+      consider({rows, columns, 1}, 2.5 + up(tiles, units) * up(blocks, 8) * (0.15 + 0.46 * loads) * (exact ? 1.3 : 1.0));
+    }
+  const double tiles128 = up((double)p.M, 128) * up(p.N, gated && !eight ? 64 : 128), rate128 = exact ? 0.85 : gated && eight ? 0.85 : 0.45;
+  for (int splits = 1; splits <= 16; splits *= 2) {
+    const int parts = parts_of(blocks, splits);
+    if (parts != splits) continue;
+    if (splits == 1) {
+      consider({128, 128, 1}, 3 + up(tiles128, units) * (blocks * rate128 + 2.5));
+    } else {
+      const double tiles = up((double)p.M, 128) * up(wide_of(p), 128) * splits, sums = (double)splits * p.M * wide_of(p);
+      consider({128, 128, splits}, 8 + up(tiles, units) * (((blocks + splits - 1) / splits + 3) / 4 * 4 * (exact ? 0.85 : 0.45) + 3) + sums * 8 / 4e6);
+    }
+  }
+  if (!exact) {
+    const double tiles = up((double)p.M, 256) * up(p.N, gated ? 128 : 256);
+    consider({256, 256, 1}, 4 + up(tiles, units) * (blocks * 1.42 + 9));
+  }
+  return best;
+}
+
+template <int TM, int TN, int ACT, int ES, bool EXACT>
 void launch_tiles(const MatmulArgs& a, hipStream_t st) {
   const int columns = ACT == SVDC_ACT_SWIGLU ? 32 * TN : 64 * TN;
   const int64_t tiles = (a.M + 64 * TM - 1) / (64 * TM) * ((a.N + columns - 1) / columns);
-  matmul8_tile_kernel<TM, TN, ACT, ES><<<(unsigned)tiles, 256, 0, st>>>(a);
+  matmul8_tile_kernel<TM, TN, ACT, ES, EXACT><<<dim3((unsigned)tiles, a.splits), 256, 0, st>>>(a);
 }
 
 // results in 8 bits need a whole block of columns in a tile of gated rows too
 template <int T, int ES>
 void launch_tiles(const MatmulArgs& a, hipStream_t st) {
   if (a.act == SVDC_ACT_SWIGLU)
-    launch_tiles<T, T == 2 && ES == 1 ? 4 : T, SVDC_ACT_SWIGLU, ES>(a, st);
+    launch_tiles<T, T == 2 && ES == 1 ? 4 : T, SVDC_ACT_SWIGLU, ES, ES == 4>(a, st);
   else if (a.act == SVDC_ACT_GELU)
-    launch_tiles<T, T, SVDC_ACT_GELU, ES>(a, st);
+    launch_tiles<T, T, SVDC_ACT_GELU, ES, ES == 4>(a, st);
   else
-    launch_tiles<T, T, SVDC_ACT_NONE, ES>(a, st);
+    launch_tiles<T, T, SVDC_ACT_NONE, ES, ES == 4>(a, st);
 }
 
 template <int TM, int TN, bool EXACT, bool GATED, bool EIGHT>
 void launch_shared(const MatmulArgs& a, hipStream_t st) {
   const int64_t tiles = (a.M + 16 * TM - 1) / (16 * TM) * ((a.N + 16 * TN - 1) / (16 * TN));
-  matmul8_shared_kernel<TM, TN, EXACT, GATED, EIGHT><<<dim3((unsigned)tiles, a.splits), kShareWaves * kWave, 0, st>>>(a);
+  matmul8_shared_kernel<TM, TN, EXACT, GATED, EIGHT><<<(unsigned)tiles, kShareWaves * kWave, 0, st>>>(a);
 }
 
-template <bool EXACT, bool GATED>
-void launch_shared(const MatmulArgs& a, int rows, hipStream_t st) {
-  if (rows == 16)
-    launch_shared<1, 4, EXACT, GATED, false>(a, st);
-  else if (rows == 32)
-    launch_shared<2, 4, EXACT, GATED, false>(a, st);
-  else
-    launch_shared<4, GATED ? 2 : 4, EXACT, GATED, false>(a, st);
-}
-
-void launch_shared(const MatmulArgs& a, int rows, hipStream_t st) {
+template <int TM, bool EXACT>
+void launch_shared(const MatmulArgs& a, int columns, hipStream_t st) {
   const bool gated = a.act == SVDC_ACT_SWIGLU;
+  if (columns == 16)
+    gated ? launch_shared<TM, 1, EXACT, true, false>(a, st) : launch_shared<TM, 1, EXACT, false, false>(a, st);
+  else if (columns == 32)
+    gated ? launch_shared<TM, 2, EXACT, true, false>(a, st) : launch_shared<TM, 2, EXACT, false, false>(a, st);
+  else
+    launch_shared<TM, 4, EXACT, false, false>(a, st);
+}
+
+void launch_shared(const MatmulArgs& a, const MatmulPlan& plan, hipStream_t st) {
   if (a.dtype == SVDC_F32)
-    gated ? launch_shared<true, true>(a, rows, st) : launch_shared<true, false>(a, rows, st);
-  else if (a.dtype == SVDC_BF16 || a.partial)
-    gated ? launch_shared<false, true>(a, rows, st) : launch_shared<false, false>(a, rows, st);
-  else if (gated)
+    plan.rows == 16 ? launch_shared<1, true>(a, plan.columns, st) : launch_shared<2, true>(a, plan.columns, st);
+  else if (a.dtype == SVDC_BF16)
+    plan.rows == 16 ? launch_shared<1, false>(a, plan.columns, st) : launch_shared<2, false>(a, plan.columns, st);
+  else if (a.act == SVDC_ACT_SWIGLU)
     launch_shared<1, 8, false, true, true>(a, st);
   else
-    rows == 16 ? launch_shared<1, 8, false, false, true>(a, st) : launch_shared<2, 8, false, false, true>(a, st);
+    plan.rows == 16 ? launch_shared<1, 8, false, false, true>(a, st) : launch_shared<2, 8, false, false, true>(a, st);
 }
 
-int32_t launch_planned(const svdc_matmul8& p, const MatmulPlan& plan, MatmulArgs a, void* workspace, hipStream_t st) {
+int32_t launch_planned(const MatmulPlan& plan, MatmulArgs a, void* workspace, hipStream_t st) {
   a.splits = plan.splits;
-  if (plan.rows == 256) {
-    p.dtype == SVDC_BF16 ? launch_tiles<4, 2>(a, st) : launch_tiles<4, 1>(a, st);
-  } else if (plan.rows == 128) {
-    p.dtype == SVDC_F32 ? launch_tiles<2, 4>(a, st) : p.dtype == SVDC_BF16 ? launch_tiles<2, 2>(a, st) : launch_tiles<2, 1>(a, st);
+  if (plan.rows <= 32) {
+    launch_shared(a, plan, st);
+  } else if (plan.rows == 256) {
+    a.dtype == SVDC_BF16 ? launch_tiles<4, 2>(a, st) : launch_tiles<4, 1>(a, st);
   } else if (plan.splits == 1) {
-    launch_shared(a, plan.rows, st);
+    a.dtype == SVDC_F32 ? launch_tiles<2, 4>(a, st) : a.dtype == SVDC_BF16 ? launch_tiles<2, 2>(a, st) : launch_tiles<2, 1>(a, st);
   } else {
-    a.partial = static_cast<float*>(workspace);
     MatmulArgs part = a;                       // plain sums of all of W's rows
-    part.N = wide_of(p);
+    part.N = a.act == SVDC_ACT_SWIGLU ? 2 * a.N : a.N;
     part.act = SVDC_ACT_NONE;
-    launch_shared(part, plan.rows, st);
+    part.bias = nullptr;
+    part.Out = workspace;
+    part.ldo = part.N;
+    a.dtype == SVDC_F32 ? launch_tiles<2, 2, SVDC_ACT_NONE, 4, true>(part, st) : launch_tiles<2, 2, SVDC_ACT_NONE, 4, false>(part, st);
     if (hipGetLastError() != hipSuccess) return SVDC_E_HIP;
-    const int64_t groups = (p.M * q8_blocks(p.N) + 15) / 16;
-    matmul8_finish_kernel<<<(unsigned)std::min<int64_t>(groups, 1 << 20), 256, 0, st>>>(a);
+    const int64_t groups = (a.M * q8_blocks(a.N) + 15) / 16;
+    matmul8_finish_kernel<<<(unsigned)std::min<int64_t>(groups, 1 << 20), 256, 0, st>>>(a, static_cast<const float*>(workspace));
   }
   return launch_status();
 }
@@ -713,8 +783,8 @@ size_t matmul8_workspace_bytes(const svdc_matmul8& p) {
 int32_t launch_matmul8(const svdc_matmul8& p, const void* A, const void* As, const void* W, const void* Ws, const float* bias, void* Out, void* Os,
                        void* workspace, hipStream_t st) {
   const MatmulArgs a{static_cast<const uint8_t*>(A), static_cast<const uint8_t*>(As), static_cast<const uint8_t*>(W), static_cast<const uint8_t*>(Ws),
-                     bias, Out, static_cast<uint8_t*>(Os), nullptr, p.M, p.ldo, p.N, p.K, p.dtype, p.act, 1};
-  return launch_planned(p, matmul8_plan(p), a, workspace, st);
+                     bias, Out, static_cast<uint8_t*>(Os), p.M, p.ldo, p.N, p.K, p.dtype, p.act, 1};
+  return launch_planned(matmul8_plan(p), a, workspace, st);
 }
 
 }  // namespace svdc
