@@ -90,10 +90,18 @@ struct NormArgs {
   float eps;
 };
 
-// Sum over the workgroup's threads, in all of them.
+// Sum over the NW waves of a row, in all of their lanes: four register moves for the 16 lanes of a DPP row, then the four rows, then the waves.
 template <int NW>
 __device__ __forceinline__ float group_sum(float v, float* part) {
-  v = wave_sum(v);
+#define SVDC_ROR_ADD(n) \
+  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + n, 0xf, 0xf, false))
+  SVDC_ROR_ADD(8);
+  SVDC_ROR_ADD(4);
+  SVDC_ROR_ADD(2);
+  SVDC_ROR_ADD(1);
+#undef SVDC_ROR_ADD
+  const auto of = [&](int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); };
+  v = (of(0) + of(16)) + (of(32) + of(48));
   if (NW == 1) return v;
   const int w = threadIdx.x / kWave;
   __syncthreads();                       // the partial sums of the row before have been read
@@ -105,9 +113,71 @@ __device__ __forceinline__ float group_sum(float v, float* part) {
   return s;
 }
 
-// One workgroup of NW waves takes a row at a time; the row is read twice, the second time out of the caches.
+// The norm of rows that fit in registers: NW waves a row, NC chunks of 8 columns a lane, all but the last of them whole.  A wave (or workgroup) takes row after row
+// and keeps the gain in registers, where it would be half as many bytes as a row of bfloat16 again.
+template <typename TX, typename TF, int NW, int NC>
+__global__ __launch_bounds__(256) void rms_norm8_rows_kernel(NormArgs a) {
+  __shared__ float part[NW];
+  constexpr int kSpan = NW * kWave * 8, ROWS = 4 / NW;       // rows of a workgroup
+  const int first = (NW == 1 ? threadIdx.x % kWave : threadIdx.x) * 8;
+  const auto left = [&](int k) { return k < NC - 1 ? 8 : a.D - (first + k * kSpan); };
+  float gain[NC][8];
+#pragma unroll
+  for (int k = 0; k < NC; ++k) {
+    if (a.gain) {
+      load8(a.gain + first + k * kSpan, left(k), gain[k]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) gain[k][i] = left(k) > i ? 1.f : 0.f;
+    }
+  }
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + (NW == 1 ? threadIdx.x / kWave : 0); row < a.rows; row += (int64_t)gridDim.x * ROWS) {
+    float h[NC][8];
+    const TX* x = static_cast<const TX*>(a.X) + row * a.ldx + first;
+#pragma unroll
+    for (int k = 0; k < NC; ++k) load8(x + k * kSpan, left(k), h[k]);
+    if (a.F) {
+      const TF* f = static_cast<const TF*>(a.F) + row * a.ldf + first;
+      float t[NC][8];
+#pragma unroll
+      for (int k = 0; k < NC; ++k) load8(f + k * kSpan, left(k), t[k]);
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[k][i] += t[k][i];
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < NC; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(h[k][i], h[k][i], sum);
+    if (a.H) {
+      TX* to = static_cast<TX*>(a.H) + row * a.ldh + first;
+#pragma unroll
+      for (int k = 0; k < NC; ++k) store8(to + k * kSpan, left(k), h[k]);
+    }
+    sum = group_sum<NW>(sum, part);
+    const float r = 1.f / sqrtf(sum / (float)a.D + a.eps);
+    uint8_t *q = a.Q + row * q8_row_bytes(a.D), *scales = a.scales + row * q8_scale_row_bytes(a.D);
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = h[k][i] * r * gain[k][i];
+      if (left(k) < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i >= left(k)) y[i] = 0.f;          // not 0 * inf, should the sum be a NaN
+      }
+      if (a.Y) store8(static_cast<TX*>(a.Y) + row * a.ldy + first + k * kSpan, left(k), y);
+      if (a.Q) store_q8(q, scales, a.D, first + k * kSpan, y);
+    }
+  }
+}
+
+// Longer rows: a workgroup of NW waves takes a row at a time and reads it twice, the second time out of the caches.
 template <typename TX, typename TF, int NW>
-__global__ __launch_bounds__(NW* kWave) void rms_norm8_kernel(NormArgs a) {
+__global__ __launch_bounds__(NW* kWave) void rms_norm8_long_kernel(NormArgs a) {
   __shared__ float part[NW];
   constexpr int kSpan = NW * kWave * 8;
   const int lane8 = threadIdx.x * 8;
@@ -152,19 +222,19 @@ __global__ __launch_bounds__(NW* kWave) void rms_norm8_kernel(NormArgs a) {
   }
 }
 
-// One wave takes 512 columns of a row.
+// One wave takes 512 columns of two rows, so that their loads are in flight together.
+constexpr int kRowsPerWave = 2;
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict__ X, uint8_t* __restrict__ Q, uint8_t* __restrict__ scales, int64_t rows,
                                                             int D, int64_t ldx) {
-  const int per_row = (D + 511) / 512;
-  const int64_t units = rows * per_row;
-  const int lane = threadIdx.x % kWave;
-  for (int64_t u = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave; u < units; u += (int64_t)gridDim.x * 4) {
-    const int64_t row = u / per_row;
-    const int c = (int)(u - row * per_row) * 512 + lane * 8;
-    float v[8];
-    load8(X + row * ldx + c, D - c, v);
-    store_q8(Q + row * q8_row_bytes(D), scales + row * q8_scale_row_bytes(D), D, c, v);
+  const int c = blockIdx.y * 512 + threadIdx.x % kWave * 8;
+  for (int64_t row0 = ((int64_t)blockIdx.x * 4 + threadIdx.x / kWave) * kRowsPerWave; row0 < rows; row0 += (int64_t)gridDim.x * 4 * kRowsPerWave) {
+    float v[kRowsPerWave][8];
+#pragma unroll
+    for (int i = 0; i < kRowsPerWave; ++i) load8(X + (row0 + i) * ldx + c, row0 + i < rows ? D - c : 0, v[i]);
+#pragma unroll
+    for (int i = 0; i < kRowsPerWave; ++i)
+      if (row0 + i < rows) store_q8(Q + (row0 + i) * q8_row_bytes(D), scales + (row0 + i) * q8_scale_row_bytes(D), D, c, v[i]);
   }
 }
 
@@ -211,13 +281,33 @@ __global__ __launch_bounds__(256) void quantize_blocks_kernel(const T* __restric
 // workgroups for `units` pieces of work, each a workgroup's turn
 unsigned grid_of(int64_t units) { return (unsigned)std::min<int64_t>(units, 1 << 20); }
 
+template <typename TX, typename TF, int NW>
+void norm_rows(const NormArgs& a, int chunks, unsigned grid, hipStream_t st) {
+  switch (chunks) {
+    case 1: rms_norm8_rows_kernel<TX, TF, NW, 1><<<grid, 256, 0, st>>>(a); break;
+    case 2: rms_norm8_rows_kernel<TX, TF, NW, 2><<<grid, 256, 0, st>>>(a); break;
+    case 3: rms_norm8_rows_kernel<TX, TF, NW, 3><<<grid, 256, 0, st>>>(a); break;
+    case 4: rms_norm8_rows_kernel<TX, TF, NW, 4><<<grid, 256, 0, st>>>(a); break;
+    case 5: rms_norm8_rows_kernel<TX, TF, NW, 5><<<grid, 256, 0, st>>>(a); break;
+    default: rms_norm8_rows_kernel<TX, TF, NW, 6><<<grid, 256, 0, st>>>(a); break;
+  }
+}
+
+// A wave a row up to 3072 columns, if that occupies the card; a workgroup of four waves up to 12288; longer rows do not fit in registers.
+template <typename TX, typename TF>
+void norm(const NormArgs& a, hipStream_t st) {
+  const int64_t units = num_compute_units();
+  if (a.D <= 6 * 512 && a.rows >= 4 * units)
+    norm_rows<TX, TF, 1>(a, (a.D + 511) / 512, (unsigned)std::min((a.rows + 3) / 4, 8 * units), st);
+  else if (a.D <= 6 * 2048)
+    norm_rows<TX, TF, 4>(a, (a.D + 2047) / 2048, (unsigned)std::min(a.rows, 8 * units), st);
+  else
+    rms_norm8_long_kernel<TX, TF, 16><<<grid_of(a.rows), 16 * kWave, 0, st>>>(a);
+}
+
 template <typename TX>
 int32_t norm_by_features(const svdc_norm8& p, const NormArgs& a, hipStream_t st) {
-  const unsigned grid = grid_of(p.rows);
-  if (p.dtype_f == SVDC_F32)
-    rms_norm8_kernel<TX, float, 4><<<grid, 4 * kWave, 0, st>>>(a);
-  else
-    rms_norm8_kernel<TX, bf16_t, 4><<<grid, 4 * kWave, 0, st>>>(a);
+  p.dtype_f == SVDC_F32 ? norm<TX, float>(a, st) : norm<TX, bf16_t>(a, st);
   return launch_status();
 }
 
@@ -226,7 +316,7 @@ int32_t quantize(const svdc_quant8& p, const void* X, void* Q, void* scales, hip
   const T* x = static_cast<const T*>(X);
   uint8_t *q = static_cast<uint8_t*>(Q), *s = static_cast<uint8_t*>(scales);
   if (p.block_rows == 1)
-    quantize_rows_kernel<T><<<grid_of((p.rows * ((p.D + 511) / 512) + 3) / 4), 256, 0, st>>>(x, q, s, p.rows, p.D, p.ldx);
+    quantize_rows_kernel<T><<<dim3(grid_of((p.rows + 4 * kRowsPerWave - 1) / (4 * kRowsPerWave)), (p.D + 511) / 512), 256, 0, st>>>(x, q, s, p.rows, p.D, p.ldx);
   else
     quantize_blocks_kernel<T><<<grid_of((p.rows + 127) / 128 * q8_blocks(p.D)), 256, 0, st>>>(x, q, s, p.rows, p.D, p.ldx);
   return launch_status();
