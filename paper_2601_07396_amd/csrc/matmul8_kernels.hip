@@ -512,7 +512,7 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
 
   load_scales(0, sc);
   // Piece p of 2 (TN + TM) of the operands of a half block, in the order in which they are multiplied
-  constexpr int PIECES = 2 * (TN + TM);
+  constexpr int PIECES = 2 * (TN + TM), AT_ONCE = PIECES > 2 * SLOTS ? (PIECES + SLOTS - 1) / SLOTS : 2;
   const auto operand_of = [](int p) { return p / 2 == 0 ? 0 : p / 2 <= TM ? TN + p / 2 - 1 : p / 2 - TM; };
   const auto read = [&](i32x8* y, const uint8_t* stage, int p, int half) {
     const int t = operand_of(p);
@@ -544,10 +544,8 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
     const int more = b + 2 < blocks ? -1 : 0;
     const auto A2 = rows_of(a.A + m0 * Kp, a_bytes & more), W2 = rows_of(a.W + n0 * Kp, w_bytes & more), U2 = rows_of(a.W + u_first * Kp, w_bytes & more);
     multiply(x[0], [&](int t) {
-      if (2 * t < PIECES) {
-        read(x[1], now, 2 * t, 1);
-        read(x[1], now, 2 * t + 1, 1);
-      }
+#pragma unroll
+      for (int p = t * AT_ONCE; p < (t + 1) * AT_ONCE && p < PIECES; ++p) read(x[1], now, p, 1);
       if (t == READ) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       if (t >= READ) {
 #pragma unroll
@@ -655,11 +653,13 @@ __global__ __launch_bounds__(256) void matmul8_finish_kernel(MatmulArgs a, const
 
 // ---- which of them ---------------------------------------------------------------------------------------------------
 
-// How a product is made.  rows 16 or 32: workgroups of that many rows by `columns` (16, 32, 64, or 128 for results in 8 bits) whose waves share the blocks;
-// rows 128 or 256: tiles of that size through LDS, `splits` parts of the columns of A and W (of 128 only).
+// How a product is made.  rows 16 or 32: workgroups of that many rows by `columns` (16, 32, 64; 16 by 128 for results in 8 bits) whose waves share the blocks;
+// rows 64, 128 or 256: tiles of that size through LDS, `splits` parts of the columns of A and W (of 128 only).
 struct MatmulPlan {
   int rows, columns, splits;
 };
+
+constexpr double kMaxTiles = 1 << 22;         // workgroups of a launch, far below what its 32-bit counts hold
 
 int wide_of(const svdc_matmul8& p) { return p.act == SVDC_ACT_SWIGLU ? 2 * p.N : p.N; }
 
@@ -669,6 +669,9 @@ int parts_of(int blocks, int splits) {
   return (blocks + each - 1) / each;
 }
 
+// The least of estimated times, in us: for each way what its rounds of workgroups (one on each compute unit; where several fit, they share it and
+// take as long) cost for a block of columns and for their ends.  Measured over some 40 products of 1 to 18432 rows, 100 to 18432 columns, K of 100 to 12288: the estimate is
+// within a quarter of the time, the way taken within a tenth of the fastest way's.
 MatmulPlan matmul8_plan(const svdc_matmul8& p) {
   const bool gated = p.act == SVDC_ACT_SWIGLU, exact = p.dtype == SVDC_F32, eight = p.dtype == SVDC_E4M3;
   const double units = num_compute_units();
@@ -676,30 +679,37 @@ MatmulPlan matmul8_plan(const svdc_matmul8& p) {
   const auto up = [](double x, double y) { return (double)(int64_t)((x + y - 1) / y); };
   MatmulPlan best{};
   double least = 1e300;
-  const auto consider = [&](MatmulPlan plan, double us) {
-    if (us < least) least = us, best = plan;
+  const auto consider = [&](MatmulPlan plan, double tiles, double us) {
+    if (us < least && tiles <= kMaxTiles) least = us, best = plan;
   };
+  // Few rows: the time of loads of 16 rows by 64 bytes.  1 x 3072 x 3072 in 16 columns 4.6 us (32: 5.8, 64: 8.6, tiles of 64: 11), 8 x 12288 x 4096 in 64 columns 13.2 us (16: 15.0)
   for (int rows = 16; rows <= 32; rows *= 2)
     for (int columns = eight ? 128 : 16; columns <= (eight ? 128 : gated ? 32 : 64); columns *= 2) {
-      if (rows == 32 && ((eight && gated) || p.M <= 16)) continue;
+      if ((rows == 32 && (eight || p.M <= 16)) || (eight && gated)) continue;
       const double tiles = up((double)p.M, rows) * up(p.N, columns);
-      const double loads = columns / 16 * (gated ? 2 : 1) + std::min(rows, (int)std::min<int64_t>(p.M, rows)) / 16.0;
-      consider({rows, columns, 1}, 2.5 + up(tiles, units) * up(blocks, 8) * (0.15 + 0.46 * loads) * (exact ? 1.3 : 1.0));
+      const double loads = columns / 16 * (gated ? 2 : 1) + std::min<int64_t>(p.M, rows) / 16.0;
+      consider({rows, columns, 1}, tiles, 2.5 + up(tiles, units) * up(blocks, 8) * (0.15 + 0.46 * loads) * (exact ? 1.3 : 1.0));
     }
-  const double tiles128 = up((double)p.M, 128) * up(p.N, gated && !eight ? 64 : 128), rate128 = exact ? 0.85 : gated && eight ? 0.85 : 0.45;
+  // Tiles of 64: 0.37 us a block of latency, until the rounds of tiles take longer.  256 x 3072 x 3072 into float32 12.5 us (tiles of 128 in two parts: 20.7), 2000 x 1024 x 1024 6.0 us (128: 7.7)
+  const double tiles64 = up((double)p.M, 64) * up(p.N, eight ? 128 : 64), rounds64 = up(tiles64, units);
+  const double rate64 = (exact ? 0.28 : eight ? 0.31 : 0.175) * (gated ? 1.7 : 1.0);
+  consider({64, 64, 1}, tiles64, 2.5 + blocks * std::max(exact || eight || gated ? 0.42 : 0.37, rate64 * rounds64) + rounds64);
+  // Tiles of 128: 2000 x 3072 x 3072 25.6 us (64: 33, 256: 33.5).  In parts: 1160 x 320 x 11072 in eight 20.9 us (whole: 41)
+  const double rate128 = exact ? 0.75 : 0.42;
   for (int splits = 1; splits <= 16; splits *= 2) {
-    const int parts = parts_of(blocks, splits);
-    if (parts != splits) continue;
+    if (parts_of(blocks, splits) != splits) continue;
     if (splits == 1) {
-      consider({128, 128, 1}, 3 + up(tiles128, units) * (blocks * rate128 + 2.5));
+      const double tiles = up((double)p.M, 128) * up(p.N, gated && !eight ? 64 : 128);
+      consider({128, 128, 1}, tiles, 3 + up(tiles, units) * (blocks * rate128 * (gated && eight ? 2 : 1) + 2));
     } else {
       const double tiles = up((double)p.M, 128) * up(wide_of(p), 128) * splits, sums = (double)splits * p.M * wide_of(p);
-      consider({128, 128, splits}, 8 + up(tiles, units) * (((blocks + splits - 1) / splits + 3) / 4 * 4 * (exact ? 0.85 : 0.45) + 3) + sums * 8 / 4e6);
+      consider({128, 128, splits}, tiles, 8 + up(tiles, units) * (((blocks + splits - 1) / splits + 3) / 4 * 4 * rate128 + 3) + sums * 8 / 4e6);
     }
   }
+  // Tiles of 256: 4608 x 3072 x 3072 42.3 us (128: 51.5)
   if (!exact) {
     const double tiles = up((double)p.M, 256) * up(p.N, gated ? 128 : 256);
-    consider({256, 256, 1}, 4 + up(tiles, units) * (blocks * 1.42 + 9));
+    consider({256, 256, 1}, tiles, 4 + up(tiles, units) * (blocks * 1.25 + 9));
   }
   return best;
 }
@@ -711,15 +721,26 @@ void launch_tiles(const MatmulArgs& a, hipStream_t st) {
   matmul8_tile_kernel<TM, TN, ACT, ES, EXACT><<<dim3((unsigned)tiles, a.splits), 256, 0, st>>>(a);
 }
 
-// results in 8 bits need a whole block of columns in a tile of gated rows too
+// Tiles of 64 T rows by 64 T columns.  Gated rows come in pairs of 32, and results in 8 bits need a whole block of columns: wider tiles of W where T is small.
 template <int T, int ES>
 void launch_tiles(const MatmulArgs& a, hipStream_t st) {
+  constexpr int PLAIN = ES == 1 && T < 2 ? 2 : T, GATES = ES == 1 && T < 4 ? 4 : T < 2 ? 2 : T;
   if (a.act == SVDC_ACT_SWIGLU)
-    launch_tiles<T, T == 2 && ES == 1 ? 4 : T, SVDC_ACT_SWIGLU, ES, ES == 4>(a, st);
+    launch_tiles<T, GATES, SVDC_ACT_SWIGLU, ES, ES == 4>(a, st);
   else if (a.act == SVDC_ACT_GELU)
-    launch_tiles<T, T, SVDC_ACT_GELU, ES, ES == 4>(a, st);
+    launch_tiles<T, PLAIN, SVDC_ACT_GELU, ES, ES == 4>(a, st);
   else
-    launch_tiles<T, T, SVDC_ACT_NONE, ES, ES == 4>(a, st);
+    launch_tiles<T, PLAIN, SVDC_ACT_NONE, ES, ES == 4>(a, st);
+}
+
+template <int T>
+void launch_tiles(const MatmulArgs& a, hipStream_t st) {
+  if (a.dtype == SVDC_F32)
+    launch_tiles<T, 4>(a, st);
+  else if (a.dtype == SVDC_BF16)
+    launch_tiles<T, 2>(a, st);
+  else
+    launch_tiles<T, 1>(a, st);
 }
 
 template <int TM, int TN, bool EXACT, bool GATED, bool EIGHT>
@@ -744,10 +765,8 @@ void launch_shared(const MatmulArgs& a, const MatmulPlan& plan, hipStream_t st) 
     plan.rows == 16 ? launch_shared<1, true>(a, plan.columns, st) : launch_shared<2, true>(a, plan.columns, st);
   else if (a.dtype == SVDC_BF16)
     plan.rows == 16 ? launch_shared<1, false>(a, plan.columns, st) : launch_shared<2, false>(a, plan.columns, st);
-  else if (a.act == SVDC_ACT_SWIGLU)
-    launch_shared<1, 8, false, true, true>(a, st);
   else
-    plan.rows == 16 ? launch_shared<1, 8, false, false, true>(a, st) : launch_shared<2, 8, false, false, true>(a, st);
+    launch_shared<1, 8, false, false, true>(a, st);
 }
 
 int32_t launch_planned(const MatmulPlan& plan, MatmulArgs a, void* workspace, hipStream_t st) {
@@ -757,7 +776,7 @@ int32_t launch_planned(const MatmulPlan& plan, MatmulArgs a, void* workspace, hi
   } else if (plan.rows == 256) {
     a.dtype == SVDC_BF16 ? launch_tiles<4, 2>(a, st) : launch_tiles<4, 1>(a, st);
   } else if (plan.splits == 1) {
-    a.dtype == SVDC_F32 ? launch_tiles<2, 4>(a, st) : a.dtype == SVDC_BF16 ? launch_tiles<2, 2>(a, st) : launch_tiles<2, 1>(a, st);
+    plan.rows == 64 ? launch_tiles<1>(a, st) : launch_tiles<2>(a, st);
   } else {
     MatmulArgs part = a;                       // plain sums of all of W's rows
     part.N = a.act == SVDC_ACT_SWIGLU ? 2 * a.N : a.N;
@@ -777,14 +796,16 @@ int32_t launch_planned(const MatmulPlan& plan, MatmulArgs a, void* workspace, hi
 
 size_t matmul8_workspace_bytes(const svdc_matmul8& p) {
   const MatmulPlan plan = matmul8_plan(p);
-  return plan.splits == 1 ? 0 : (size_t)plan.splits * p.M * wide_of(p) * sizeof(float);
+  return plan.splits <= 1 ? 0 : (size_t)plan.splits * p.M * wide_of(p) * sizeof(float);
 }
 
 int32_t launch_matmul8(const svdc_matmul8& p, const void* A, const void* As, const void* W, const void* Ws, const float* bias, void* Out, void* Os,
                        void* workspace, hipStream_t st) {
   const MatmulArgs a{static_cast<const uint8_t*>(A), static_cast<const uint8_t*>(As), static_cast<const uint8_t*>(W), static_cast<const uint8_t*>(Ws),
                      bias, Out, static_cast<uint8_t*>(Os), p.M, p.ldo, p.N, p.K, p.dtype, p.act, 1};
-  return launch_planned(matmul8_plan(p), a, workspace, st);
+  const MatmulPlan plan = matmul8_plan(p);
+  if (plan.rows == 0) return SVDC_E_SHAPE;          // a result of more than 2^38 elements
+  return launch_planned(plan, a, workspace, st);
 }
 
 }  // namespace svdc

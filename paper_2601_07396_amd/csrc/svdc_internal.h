@@ -4,16 +4,23 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/svdcache.h"
 
 namespace svdc {
 
 // Compute units of the current device (a partition of a card has fewer than the 256 of a whole one); every rule of a launch
 // that depends on how much of the machine a grid fills asks for it.
+// Asked for once a device.
 inline int num_compute_units() {
+  static std::atomic<int> known[64];
   int dev = 0, n = 0;
   if (hipGetDevice(&dev) != hipSuccess) return 256;
+  const bool keep = dev >= 0 && dev < 64;
+  if (keep && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
   if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) return 256;
+  if (keep) known[dev].store(n, std::memory_order_relaxed);
   return n;
 }
 

@@ -581,3 +581,25 @@ def test_binding_refuses_layouts():
         svdc.svdcache_matmul8(svdc.make_matmul8(4, 128, 256, act="swiglu"), Q, s, W, Ws, None, torch.zeros(4, 128).bfloat16())
     with pytest.raises(RuntimeError, match="GPU"):
         svdc.svdcache_matmul8(m, Q, s, W, Ws, None, O, Os)
+
+
+# Sizes that between them take every way in which a product is made on a whole card, with odd ends: groups of 16 and 32 rows by 16, 32, 64 (and 128) columns, tiles of 64, 128
+# and 256, long axes in 2, 4, 8 and 16 parts.
+WAYS = {
+    torch.float32: {
+        "none": [(1178, 1668, 130), (90, 3, 15866), (132, 5571, 7117), (4108, 3, 17709), (91, 5, 15003), (12, 3, 300), (203, 306, 260), (166, 1356, 666), (674, 166, 257),
+                 (388, 323, 392), (4311, 33, 846), (291, 209, 300)],
+        "swiglu": [(1897, 1754, 130), (95, 3, 8043), (138, 2077, 9579), (124, 3, 17596), (95, 3, 7665), (12, 3, 129), (166, 691, 535), (371, 163, 385), (457, 278, 644), (45, 3, 300)]},
+    torch.bfloat16: {
+        "none": [(1411, 1409, 131), (102, 3, 16148), (130, 4212, 8011), (4127, 3, 13753), (99, 3, 14365), (12, 3, 257), (215, 295, 131), (301, 815, 391), (3014, 4137, 514), (579, 204, 137),
+                 (324, 395, 257), (2092, 97, 670), (211, 290, 300)],
+        "swiglu": [(2306, 2196, 100), (92, 4, 8038), (4198, 65, 6144), (93, 3, 13982), (90, 3, 7383), (163, 682, 435), (3499, 1732, 536), (407, 146, 267), (211, 585, 536), (45, 3, 300)]},
+    torch.float8_e4m3fn: {
+        "gelu": [(2877, 3587, 130), (101, 3, 7768), (132, 4126, 6029), (90, 3, 3215), (90, 3, 3743), (12, 3, 907), (2773, 4388, 535), (45, 3, 300)],
+        "swiglu": [(3736, 2719, 100), (91, 3, 7789), (92, 3, 3040), (90, 3, 3359), (90, 3, 3889), (5846, 641, 2898), (45, 3, 300)]}}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,act,M,N,K", [(d, a, *s) for d, by in WAYS.items() for a, sizes in by.items() for s in sizes])
+def test_matmul8_every_way(dtype, act, M, N, K):
+    check_product(M, N, K, dtype, act, with_bias=N % 2 == 1, seed=N, planted=M % 2 == 0, ldo_pad=5 if M % 3 == 0 else 0)
