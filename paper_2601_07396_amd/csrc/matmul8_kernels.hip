@@ -298,22 +298,20 @@ __device__ __forceinline__ void store16(void* Out, int64_t at, int n, const u32x
   }
 }
 
-// A wave's finished 32 rows v[i][4 q + e] = Out[row lane % 32][column 32 i + 8 q + 4 (lane / 32) + e] go to memory through its own part of LDS, so that it writes
-// whole lines.  inv: of the scale of the lane's row, for 8 bits.
+// Finished rows of a wave, v[i][4 q + e] = Out[row lane % 32][column 32 i + 8 q + 4 (lane / 32) + e], go to memory through its own part of LDS, so that it writes whole
+// lines: rows_to_lds puts 32 of them there (inv: of the scale of the lane's row, for 8 bits), rows_to_memory takes them on.
 template <int TO, int ES>
-__device__ __forceinline__ void store_rows(const MatmulArgs& a, const float (&v)[TO][16], int64_t m_first, int col_first, int lane, float inv, uint8_t* lds) {
-  constexpr int RB = TO * 32 * ES, CH = RB / 16, PER = 64 / CH;
+__device__ __forceinline__ void rows_to_lds(const float (&v)[TO][16], int lane, float inv, uint8_t* lds) {
+  constexpr int RB = TO * 32 * ES, CH = RB / 16;
   static_assert(RB <= 256, "");
   const int r = lane % 32, h = lane / 32;
-  const int64_t ldo = ES == 1 ? q8_row_bytes(a.N) : a.ldo;
-  const int end = ES == 1 ? (int)q8_row_bytes(a.N) : a.N;
 #pragma unroll
   for (int i = 0; i < TO; ++i)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int byte = (32 * i + 8 * q + 4 * h) * ES;
       uint8_t* to = lds + r * RB + (byte / 16 ^ (r & (CH - 1))) * 16 + byte % 16;
-      const float *t = v[i] + 4 * q;
+      const float* t = v[i] + 4 * q;
       if (ES == 4)
         *reinterpret_cast<f32x4*>(to) = f32x4{t[0], t[1], t[2], t[3]};
       else if (ES == 2)
@@ -321,72 +319,107 @@ __device__ __forceinline__ void store_rows(const MatmulArgs& a, const float (&v)
       else
         *reinterpret_cast<uint32_t*>(to) = pack_e4m3(t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv);
     }
-  asm volatile("" ::: "memory");           // a wave's LDS operations are carried out in order
-#pragma unroll
-  for (int p = 0; p < 32 / PER; ++p) {
-    const int row = p * PER + lane / CH, chunk = lane % CH;
-    const u32x4 w = *reinterpret_cast<const u32x4*>(lds + row * RB + (chunk ^ (row & (CH - 1))) * 16);
-    const int col = col_first + chunk * 16 / ES;
-    if (m_first + row < a.M && col < end) store16<ES>(a.Out, (m_first + row) * ldo + col, end - col, w);
-  }
-  asm volatile("" ::: "memory");
 }
 
-// A wave's sums c (bias included; gated: c[TO + i] is what c[i] gates) to Out.  lds: 32 * 32 TO * 4 bytes a wave at most; part: 4 * 32 floats.  Called by all
-// waves of the workgroup.  edge: the tile reaches beyond column N.
+template <int TO, int ES>
+__device__ __forceinline__ void rows_to_memory(const MatmulArgs& a, int64_t m_first, int col_first, bool inside, int lane, const uint8_t* lds) {
+  constexpr int RB = TO * 32 * ES, CH = RB / 16, PER = 64 / CH;
+  const int64_t ldo = ES == 1 ? q8_row_bytes(a.N) : a.ldo;
+  const int end = ES == 1 ? (int)q8_row_bytes(a.N) : a.N;
+  const int row0 = lane / CH, chunk = lane % CH, col = col_first + chunk * 16 / ES;
+  u32x4 w[32 / PER];
+#pragma unroll
+  for (int p = 0; p < 32 / PER; ++p) {
+    const int row = p * PER + row0;
+    w[p] = *reinterpret_cast<const u32x4*>(lds + row * RB + (chunk ^ (row & (CH - 1))) * 16);
+  }
+  const int64_t at = (m_first + row0) * ldo + col;
+  if (inside) {
+#pragma unroll
+    for (int p = 0; p < 32 / PER; ++p) store16<ES>(a.Out, at + p * PER * ldo, 16 / ES, w[p]);
+  } else {
+#pragma unroll
+    for (int p = 0; p < 32 / PER; ++p)
+      if (m_first + p * PER + row0 < a.M && col < end) store16<ES>(a.Out, at + p * PER * ldo, end - col, w[p]);
+  }
+}
+
+// A wave's sums c (bias included; gated: c[TO + i] is what c[i] gates) to Out, JP tiles of 32 rows at a time: one wave a SIMD has nothing to hide the ways
+// through LDS behind but another tile.  lds: JP * 32 * 32 TO ES bytes a wave; part: 4 * 32 JP floats.  Called by all waves of the workgroup.  inside: the tile lies within Out;
+// last: it holds the last column.
 template <int TM, int TN, int ACT, int ES, typename Acc>
-__device__ __forceinline__ void store_tile(const MatmulArgs& a, Acc& c, int64_t m0, int n0, bool edge, int wm, int wn, int lane, uint8_t* lds,
+__device__ __forceinline__ void store_tile(const MatmulArgs& a, Acc& c, int64_t m0, int n0, bool inside, bool last, int wm, int wn, int lane, uint8_t* lds,
                                            float* part) {
   constexpr bool GATED = ACT == SVDC_ACT_SWIGLU;
-  constexpr int TO = GATED ? TN / 2 : TN;
+  constexpr int TO = GATED ? TN / 2 : TN, JP = TM > 1 && ES < 4 ? 2 : 1;
   constexpr bool SHARED = ES == 1 && TO < 4;        // the two waves of the columns share their scales
   const int h = lane / 32, col_first = n0 + wn * 32 * TO;
-  uint8_t* mine = lds + (wn * 2 + wm) * (32 * 32 * TO * ES);
+  uint8_t* mine = lds + (wn * 2 + wm) * (JP * 32 * 32 * TO * ES);
 #pragma unroll
-  for (int j = 0; j < TM; ++j) {
-    const int64_t m_first = m0 + wm * 32 * TM + 32 * j;
+  for (int j0 = 0; j0 < TM; j0 += JP) {
 #pragma unroll
-    for (int i = 0; i < TN; ++i) hold(c[i][j]);      // 32 rows after the other, not all in registers at once
-    float v[TO][16];
+    for (int j = 0; j < JP; ++j)
 #pragma unroll
-    for (int i = 0; i < TO; ++i)
+      for (int i = 0; i < TN; ++i) hold(c[i][j0 + j]);      // these rows after the ones before, not all in registers at once
+    const int64_t m_first = m0 + wm * 32 * TM + 32 * j0;
+    float v[JP][TO][16], inv[JP];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float z = c[i][j][e];
-        v[i][e] = ACT == SVDC_ACT_GELU ? gelu(z) : GATED ? silu(z) * c[TO + i][j][e] : z;
-      }
-    float inv = 1.f;
-    if (ES == 1) {
-      if (edge) {
-#pragma unroll
-        for (int i = 0; i < TO; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (col_first + 32 * i + e / 4 * 8 + 4 * h + e % 4 >= a.N) v[i][e] = 0.f;
-      }
-      float top = 0.f;
+    for (int j = 0; j < JP; ++j)
 #pragma unroll
       for (int i = 0; i < TO; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(v[i][e]));
-      top = fmaxf(top, __shfl_xor(top, 32));
+        for (int e = 0; e < 16; ++e) {
+          const float z = c[i][j0 + j][e];
+          v[j][i][e] = ACT == SVDC_ACT_GELU ? gelu(z) : GATED ? silu(z) * c[TO + i][j0 + j][e] : z;
+        }
+    if (ES == 1) {
+      float top[JP];
+#pragma unroll
+      for (int j = 0; j < JP; ++j) {
+        if (!inside) {
+#pragma unroll
+          for (int i = 0; i < TO; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (col_first + 32 * i + e / 4 * 8 + 4 * h + e % 4 >= a.N) v[j][i][e] = 0.f;
+        }
+        float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < TO; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) t[e / 4] = fmaxf(t[e / 4], fabsf(v[j][i][e]));
+        const float u = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(u), __float_as_uint(u), false, false);   // the two halves of the wave
+        top[j] = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+      }
       if (SHARED) {
         __syncthreads();                   // the maxima of the rows before have been read
-        part[(wn * 2 + wm) * 32 + lane % 32] = top;
+#pragma unroll
+        for (int j = 0; j < JP; ++j) part[((wn * 2 + wm) * JP + j) * 32 + lane % 32] = top[j];
         __syncthreads();
-        top = fmaxf(top, part[((wn ^ 1) * 2 + wm) * 32 + lane % 32]);
+#pragma unroll
+        for (int j = 0; j < JP; ++j) top[j] = fmaxf(top[j], part[(((wn ^ 1) * 2 + wm) * JP + j) * 32 + lane % 32]);
       }
-      const int byte = scale_byte(top);
-      inv = inverse_scale(byte);
       const int block = (SHARED ? n0 : col_first) / kScaleBlock, blocks = q8_blocks(a.N), row_bytes = q8_scale_row_bytes(a.N);
-      if (lane < 32 && m_first + lane < a.M) {
-        uint8_t* to = a.Os + (m_first + lane) * row_bytes;
-        if (block < blocks && !(SHARED && wn)) to[block] = (uint8_t)byte;
-        if (edge && wn)
-          for (int b = blocks; b < row_bytes; ++b) to[b] = 127;
+#pragma unroll
+      for (int j = 0; j < JP; ++j) {
+        const int byte = scale_byte(top[j]);
+        inv[j] = inverse_scale(byte);
+        const int64_t m = m_first + 32 * j + lane;
+        if (lane < 32 && m < a.M) {
+          uint8_t* to = a.Os + m * row_bytes;
+          if (block < blocks && !(SHARED && wn)) to[block] = (uint8_t)byte;
+          if (last && wn)
+            for (int b = blocks; b < row_bytes; ++b) to[b] = 127;
+        }
       }
     }
-    store_rows<TO, ES>(a, v, m_first, col_first, lane, inv, mine);
+#pragma unroll
+    for (int j = 0; j < JP; ++j) rows_to_lds<TO, ES>(v[j], lane, ES == 1 ? inv[j] : 1.f, mine + j * (32 * 32 * TO * ES));
+    asm volatile("" ::: "memory");         // a wave's LDS operations are carried out in order
+#pragma unroll
+    for (int j = 0; j < JP; ++j) rows_to_memory<TO, ES>(a, m_first + 32 * j, col_first, inside, lane, mine + j * (32 * 32 * TO * ES));
+    asm volatile("" ::: "memory");
   }
 }
 
@@ -583,8 +616,8 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
     }
   }
   asm volatile("s_waitcnt lgkmcnt(0) vmcnt(0)\n\ts_barrier" ::: "memory");
-  const bool edge = n0 + columns > a.N || column_tile == column_tiles - 1;
-  store_tile<TM, TN, ACT, ES>(a, c, m0, n0, edge, wm, wn, lane, stage0.b, reinterpret_cast<float*>(stage1.b));
+  const bool inside = m0 + BM <= a.M && n0 + columns <= a.N;
+  store_tile<TM, TN, ACT, ES>(a, c, m0, n0, inside, column_tile == column_tiles - 1, wm, wn, lane, stage0.b, reinterpret_cast<float*>(stage1.b));
 }
 
 // ACT: svdc_act;  ES: bytes of an element of Out;  EXACT: float32 sums.  Part blockIdx.y of a.splits of the columns of A and W
