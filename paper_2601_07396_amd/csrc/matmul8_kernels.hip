@@ -10,7 +10,6 @@
 // float32.  That is about 4e-5 of a result: nothing beside the rounding of a result to bfloat16 or e4m3, but not float32.  Results in float32 are made with
 // bfloat16 instructions, at half the rate: e4m3 values times powers of two are bfloat16 values exactly, and those products are summed with 24 bits.
 #include <algorithm>
-#include <type_traits>
 
 #include "eight_bit.h"
 #include "svdc_internal.h"
@@ -30,13 +29,13 @@ struct MatmulArgs {
   int N, K, dtype, act, splits;
 };
 
-__device__ __forceinline__ f32x4 mfma8(const i32x8& w, const i32x8& a, const f32x4& c, int sw, int sa) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, sw, 0, sa);
+// blocks of each of `splits` parts of the columns of A and W: a multiple of four, as scales are read four at a time; the last part may have fewer
+__host__ __device__ __forceinline__ int blocks_of_part(int blocks, int splits) {
+  return splits == 1 ? blocks : ((blocks + splits - 1) / splits + 3) / 4 * 4;
 }
 
-__device__ __forceinline__ i32x8 load32(const uint8_t* p) {
-  const u32x4 lo = reinterpret_cast<const u32x4*>(p)[0], hi = reinterpret_cast<const u32x4*>(p)[1];
-  return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+__device__ __forceinline__ f32x4 mfma8(const i32x8& w, const i32x8& a, const f32x4& c, int sw, int sa) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, sw, 0, sa);
 }
 
 // 8 e4m3 values times 2^(byte - 127) as bfloat16, exactly
@@ -80,6 +79,10 @@ __device__ __forceinline__ float finished(const MatmulArgs& a, int col, float z,
 // Where there are not enough large tiles to occupy the card, a workgroup makes 16 TM rows by 16 TN columns and its eight waves share the blocks of columns of
 // A and W: wave w takes blocks w, w + 8, ... straight from memory into registers (nothing is used twice within a wave), and the eight sums are added through
 // LDS, always in the same order.
+//
+// What bounds it: the look-ups of lines by the loads.  A load of an operand takes 64 bytes of 16 rows, and lines are looked up one at a time: 54 MB of weights in this
+// pattern take 13.6 us alone, in 128 bytes of 8 rows 9.8 us, but the matrix instructions want 16 rows (instructions that waste half their work on the other pattern were no
+// faster).  1 x 18432 x 3072 into bfloat16 12.1 us (4.7 TB/s of weights; a read of as many bytes 8.7 us), 1 x 3072 x 3072 4.6 us.
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }   // a value that all lanes hold, as a scalar
 
@@ -260,9 +263,14 @@ __global__ __launch_bounds__(kShareWaves* kWave) void matmul8_shared_kernel(Matm
 // ---- tiles ----------------------------------------------------------------------------------------------------------
 //
 // A workgroup of four waves makes BM = 64 TM rows by BN = 64 TN rows of W; a wave 32 TM by 32 TN of them, with 32 x 32 x 64 instructions (the same rate as
-// 16 x 16 x 128, half the operand words).  Two stages of 128 columns of both operands lie in LDS, written by direct loads one block ahead; a wave's operands
+// 16 x 16 x 128, half the operand words).  Two or four stages of 128 columns of both operands lie in LDS, written by direct loads one or three blocks ahead; a wave's operands
 // lie in two register sets, one read from LDS while the other is multiplied.  Rows of 128 bytes are eight 16-byte slots; slot s of row r holds columns
 // 16 (s ^ swizzle(r)): eight consecutive rows and the rows of one parity of sixteen have different slots of a column, so that reads meet no bank twice.
+//
+// What bounds it.  Tiles of 256, one workgroup on a compute unit: the matrix cores and their clock, which the card lowers under this load to 1.76 GHz: 4608 x 3072 x 12288 147 us,
+// 2370 TFLOP/s, matrix cores 83 % busy; and the tile's ends, when they stand still (first loads 3.5 us, sums to results 4 us, GELU 3.5 us, stores 2-5 us a tile, all units at once): 18432 x 12288 x
+// 3072 with GELU into 8 bits 588 us, 2370 TFLOP/s, 63 % busy.  Tiles of 64 and 128: the latency of loads for each block, less of it with four stages (where they pay: see
+// deep() below).  Results in float32: widening, 64 conversions a block and wave; 256 x 3072 x 3072 12.2 us, 22 % busy.
 __device__ __forceinline__ int swizzle(int row) { return (row & 7) ^ (row >> 3 & 1); }
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -445,7 +453,7 @@ __device__ __forceinline__ void tile_at(int id, int row_tiles, int column_tiles,
   column = uniform(at / high);
 }
 
-template <int TM, int TN, int ACT, int ES, bool EXACT>
+template <int TM, int TN, int ACT, int ES, bool EXACT, int STAGES>
 __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
   constexpr bool GATED = ACT == SVDC_ACT_SWIGLU;
   constexpr int BM = 64 * TM, BN = 64 * TN, LOADS = (BM + BN) / 32;
@@ -455,20 +463,21 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
   constexpr int SLOTS = TM * TN, READ = SLOTS == 16 ? 10 : SLOTS - 1, FIRST = SLOTS == 16 ? 6 : LOADS / 2, LATE = SLOTS == 16 ? 10 : SLOTS;
   __shared__ TileStage<TM, TN> stage0;
   __shared__ TileStage<TM, TN> stage1;
+  __shared__ TileStage<TM, TN> stage2;           // not there with two stages
+  __shared__ TileStage<TM, TN> stage3;
+  uint8_t* const stages[4] = {stage0.b, stage1.b, STAGES == 4 ? stage2.b : stage0.b, STAGES == 4 ? stage3.b : stage1.b};
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int wm = wave & 1, wn = wave >> 1;
-  constexpr bool gated = GATED;
   const int64_t Kp = q8_row_bytes(a.K);
   const int ss = uniform(q8_scale_row_bytes(a.K));
-  // this part's blocks of columns of A and W: a multiple of four each, as scales are read four at a time
-  const int all = q8_blocks(a.K), each = ((all + a.splits - 1) / a.splits + 3) / 4 * 4, skip = uniform(a.splits == 1 ? 0 : blockIdx.y * each);
-  const int blocks = uniform(a.splits == 1 ? all : min(each, all - skip));
+  const int all = q8_blocks(a.K), each = blocks_of_part(all, a.splits), skip = uniform(blockIdx.y * each);      // this part's blocks of columns of A and W
+  const int blocks = uniform(min(each, all - skip));
   a.A += (int64_t)skip * 128;
   a.W += (int64_t)skip * 128;
   a.As += skip;
   a.Ws += skip;
   if (ES == 4) a.Out = static_cast<float*>(a.Out) + blockIdx.y * a.M * a.ldo;
-  const int columns = gated ? BN / 2 : BN;                  // of Out
+  const int columns = GATED ? BN / 2 : BN;                  // of Out
   const int column_tiles = (a.N + columns - 1) / columns;
   const int row_tiles = (int)((a.M + BM - 1) / BM);
   int row_tile, column_tile;
@@ -479,17 +488,16 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
   // row of W behind row i of the tile; rows beyond the last are read as the last one, and what they give is not stored.  Gated: a wave's first 16 TN
   // rows are gates, its others what they multiply
   const auto w_row = [&](int i) {
-    if (!gated) return (int64_t)min(n0 + i, a.N - 1);
+    if (!GATED) return (int64_t)min(n0 + i, a.N - 1);
     const int w = i / (32 * TN), j = i % (32 * TN), up = j / (16 * TN);
     return (int64_t)min(n0 + w * 16 * TN + j % (16 * TN), a.N - 1) + (up ? a.N : 0);
   };
   const auto a_row = [&](int i) { return min(m0 + i, a.M - 1); };
 
   // This wave's pieces of 8 rows of a stage: bounds-checked loads from A, the gates and what they multiply, each from the tile's first row on
-  const auto rows_of = [](const uint8_t* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, bytes, 0x00027000); };
   const int a_bytes = uniform((int)(min<int64_t>(BM, a.M - m0) * Kp - skip * 128)), w_bytes = uniform((int)(min(columns, a.N - n0) * Kp - skip * 128));
-  const int64_t u_first = (gated ? (int64_t)a.N : 0) + n0;
-  const auto A1 = rows_of(a.A + m0 * Kp, a_bytes), W1 = rows_of(a.W + n0 * Kp, w_bytes), U1 = rows_of(a.W + u_first * Kp, w_bytes);
+  const int64_t u_first = (GATED ? (int64_t)a.N : 0) + n0;
+  const auto A1 = bounded(a.A + m0 * Kp, a_bytes), W1 = bounded(a.W + n0 * Kp, w_bytes), U1 = bounded(a.W + u_first * Kp, w_bytes);
   const auto is_up = [](int j) { return GATED && (j * 32 - BM) % (32 * TN) >= 16 * TN; };
   uint32_t from[LOADS];
 #pragma unroll
@@ -507,7 +515,7 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
   const int a_base = (wm * 32 * TM + r) * 128, w_base = (BM + wn * 32 * TN + r) * 128;
 
   // scales of four blocks at a time, those of the current block in the lowest byte
-  const auto As = rows_of(a.As + m0 * ss, uniform((int)min<int64_t>(BM, a.M - m0) * ss - skip)), Ws = rows_of(a.Ws, uniform(q8_blocks(gated ? 2 * a.N : a.N) * ss - skip));
+  const auto As = bounded(a.As + m0 * ss, uniform((int)min<int64_t>(BM, a.M - m0) * ss - skip)), Ws = bounded(a.Ws, uniform(q8_blocks(GATED ? 2 * a.N : a.N) * ss - skip));
   uint32_t scale_row[TN + TM];
 #pragma unroll
   for (int t = 0; t < TN; ++t) scale_row[t] = (uint32_t)(w_row(wn * 32 * TN + t * 32 + r) / kScaleBlock * ss);
@@ -520,23 +528,23 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
   };
 
 #pragma unroll
-  for (int j = 0; j < LOADS; ++j) load(j, 0, stage0.b, A1, W1, U1);
-  if (blocks > 1) {
+  for (int s = 0; s < STAGES; ++s)
+    if (s < blocks) {
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) load(j, 1, stage1.b, A1, W1, U1);
-  }
+      for (int j = 0; j < LOADS; ++j) load(j, s, stages[s], A1, W1, U1);
+    }
   // the sums start at the bias: bounds-checked loads, zero beyond the last column and without one
   const uint8_t* const bias_bytes = reinterpret_cast<const uint8_t*>(a.bias);
-  const auto bias_z = rows_of(bias_bytes, uniform(a.bias ? a.N * 4 : 0)),
-             bias_u = rows_of(bias_bytes + (gated ? (int64_t)a.N * 4 : 0), uniform(a.bias ? a.N * 4 : 0));
+  const auto bias_z = bounded(bias_bytes, uniform(a.bias ? a.N * 4 : 0)),
+             bias_u = bounded(bias_bytes + (GATED ? (int64_t)a.N * 4 : 0), uniform(a.bias ? a.N * 4 : 0));
   f32x16 c[TN][TM];
 #pragma unroll
   for (int i = 0; i < TN; ++i) {
     f32x16 bias;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int col = n0 + wn * 32 * (gated ? TN / 2 : TN) + 32 * (gated ? i % (TN / 2) : i) + e / 4 * 8 + 4 * h + e % 4;
-      bias[e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(gated && i >= TN / 2 ? bias_u : bias_z, col * 4, 0, 0));
+      const int col = n0 + wn * 32 * (GATED ? TN / 2 : TN) + 32 * (GATED ? i % (TN / 2) : i) + e / 4 * 8 + 4 * h + e % 4;
+      bias[e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(GATED && i >= TN / 2 ? bias_u : bias_z, col * 4, 0, 0));
     }
 #pragma unroll
     for (int j = 0; j < TM; ++j) c[i][j] = bias;
@@ -558,7 +566,7 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
   arrived(sc);
   __syncthreads();
 #pragma unroll
-  for (int p = 0; p < PIECES; ++p) read(x[0], stage0.b, p, 0);
+  for (int p = 0; p < PIECES; ++p) read(x[0], stages[0], p, 0);
 
   const auto multiply = [&](const i32x8* y, auto&& between) {
 #pragma unroll
@@ -571,27 +579,27 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
         __builtin_amdgcn_sched_barrier(0);
       }
   };
-  // Block b lies in `now` with its first half in x[0].  Once all waves have read its second half, block b + 2 is loaded there; beyond the last one the
+  // Block b lies in `now` with its first half in x[0].  Once all waves have read its second half, block b + STAGES is loaded there; beyond the last one the
   // loads are out of bounds and fetch nothing.
   const auto block = [&](int b, uint8_t* now, uint8_t* then) {
-    const int more = b + 2 < blocks ? -1 : 0;
-    const auto A2 = rows_of(a.A + m0 * Kp, a_bytes & more), W2 = rows_of(a.W + n0 * Kp, w_bytes & more), U2 = rows_of(a.W + u_first * Kp, w_bytes & more);
+    const int more = b + STAGES < blocks ? -1 : 0;
+    const auto A2 = bounded(a.A + m0 * Kp, a_bytes & more), W2 = bounded(a.W + n0 * Kp, w_bytes & more), U2 = bounded(a.W + u_first * Kp, w_bytes & more);
     multiply(x[0], [&](int t) {
 #pragma unroll
       for (int p = t * AT_ONCE; p < (t + 1) * AT_ONCE && p < PIECES; ++p) read(x[1], now, p, 1);
       if (t == READ) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       if (t >= READ) {
 #pragma unroll
-        for (int j = (t - READ) * FIRST / (SLOTS - READ); j < (t - READ + 1) * FIRST / (SLOTS - READ); ++j) load(j, b + 2, now, A2, W2, U2);
+        for (int j = (t - READ) * FIRST / (SLOTS - READ); j < (t - READ + 1) * FIRST / (SLOTS - READ); ++j) load(j, b + STAGES, now, A2, W2, U2);
       }
     });
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(FIRST) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STAGES - 2) * LOADS + FIRST) : "memory");
     multiply(x[1], [&](int t) {
 #pragma unroll
       for (int p = t * PIECES / SLOTS; p < (t + 1) * PIECES / SLOTS; ++p) read(x[0], then, p, 0);
       if (t < LATE) {
 #pragma unroll
-        for (int j = FIRST + t * (LOADS - FIRST) / LATE; j < FIRST + (t + 1) * (LOADS - FIRST) / LATE; ++j) load(j, b + 2, now, A2, W2, U2);
+        for (int j = FIRST + t * (LOADS - FIRST) / LATE; j < FIRST + (t + 1) * (LOADS - FIRST) / LATE; ++j) load(j, b + STAGES, now, A2, W2, U2);
       }
     });
 #pragma unroll
@@ -600,19 +608,17 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
   int b = 0;
   for (; b + 3 < blocks; b += 4) {
     load_scales(min(b + 4, ss - skip - 4), next_sc);
-    block(b, stage0.b, stage1.b);
-    block(b + 1, stage1.b, stage0.b);
-    block(b + 2, stage0.b, stage1.b);
-    block(b + 3, stage1.b, stage0.b);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) block(b + d, stages[d], stages[(d + 1) % 4]);
     arrived(next_sc);
 #pragma unroll
     for (int t = 0; t < TN + TM; ++t) sc[t] = next_sc[t];
   }
   if (b < blocks) {
-    block(b, stage0.b, stage1.b);
+    block(b, stages[0], stages[1]);
     if (b + 1 < blocks) {
-      block(b + 1, stage1.b, stage0.b);
-      if (b + 2 < blocks) block(b + 2, stage0.b, stage1.b);
+      block(b + 1, stages[1], stages[2]);
+      if (b + 2 < blocks) block(b + 2, stages[2], stages[3]);
     }
   }
   asm volatile("s_waitcnt lgkmcnt(0) vmcnt(0)\n\ts_barrier" ::: "memory");
@@ -620,11 +626,11 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
   store_tile<TM, TN, ACT, ES>(a, c, m0, n0, inside, column_tile == column_tiles - 1, wm, wn, lane, stage0.b, reinterpret_cast<float*>(stage1.b));
 }
 
-// ACT: svdc_act;  ES: bytes of an element of Out;  EXACT: float32 sums.  Part blockIdx.y of a.splits of the columns of A and W
-template <int TM, int TN, int ACT, int ES, bool EXACT>
+// ACT: svdc_act;  ES: bytes of an element of Out;  EXACT: float32 sums;  STAGES: blocks in LDS, 2 or 4.  Part blockIdx.y of a.splits of the columns of A and W
+template <int TM, int TN, int ACT, int ES, bool EXACT, int STAGES>
 __global__ __launch_bounds__(256) void matmul8_tile_kernel(MatmulArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__          // buffer descriptors and accumulation registers mean nothing to the host's pass
-  tile_of_product<TM, TN, ACT, ES, EXACT>(a);
+  tile_of_product<TM, TN, ACT, ES, EXACT, STAGES>(a);
 #endif
 }
 
@@ -696,15 +702,20 @@ constexpr double kMaxTiles = 1 << 22;         // workgroups of a launch, far bel
 
 int wide_of(const svdc_matmul8& p) { return p.act == SVDC_ACT_SWIGLU ? 2 * p.N : p.N; }
 
-// parts of the columns of A and W of which none is empty: a tile takes a multiple of four blocks
-int parts_of(int blocks, int splits) {
-  const int each = ((blocks + splits - 1) / splits + 3) / 4 * 4;
-  return (blocks + each - 1) / each;
-}
+// parts of the columns of A and W of which none is empty
+int parts_of(int blocks, int splits) { return (blocks + blocks_of_part(blocks, splits) - 1) / blocks_of_part(blocks, splits); }
+
+// Whether tiles of 64 TM by 64 TN with sums of `blocks` blocks have four stages in LDS instead of two: where all of them are at work at once all the same and the sums
+// are long enough.  256 x 3072 x 3072 into bfloat16, 192 tiles of 64: 8.9 us with four, 11.7 with two; 512 x 12288 x 3072, 1536 tiles: 35 and 27; 448 x 4096 x 1024:
+// 6.1 and 5.9.  With float32 sums a block takes its time from widening the operands (256 x 3072 x 3072 12.5 us with either): two.
+constexpr int kUnitLds = 160 << 10, kDeepLds = 128 << 10;
+constexpr int tile_lds(int TM, int TN, int stages) { return stages * 64 * (TM + TN) * 128; }
+constexpr bool can_be_deep(int TM, int TN, bool exact) { return !exact && tile_lds(TM, TN, 4) <= kDeepLds; }
+bool deep(double tiles, int blocks, int TM, int TN) { return blocks > 8 && tiles <= (double)num_compute_units() * (kUnitLds / tile_lds(TM, TN, 4)); }
 
 // The least of estimated times, in us: for each way what its rounds of workgroups (one on each compute unit; where several fit, they share it and
 // take as long) cost for a block of columns and for their ends.  Measured over some 40 products of 1 to 18432 rows, 100 to 18432 columns, K of 100 to 12288: the estimate is
-// within a quarter of the time, the way taken within a tenth of the fastest way's.
+// within a quarter of the time, the way taken mostly within a twentieth and at most a sixth (32 x 4096 x 4096, gated) above the fastest way's.
 MatmulPlan matmul8_plan(const svdc_matmul8& p) {
   const bool gated = p.act == SVDC_ACT_SWIGLU, exact = p.dtype == SVDC_F32, eight = p.dtype == SVDC_E4M3;
   const double units = num_compute_units();
@@ -715,7 +726,8 @@ MatmulPlan matmul8_plan(const svdc_matmul8& p) {
   const auto consider = [&](MatmulPlan plan, double tiles, double us) {
     if (us < least && tiles <= kMaxTiles) least = us, best = plan;
   };
-  // Few rows: the time of loads of 16 rows by 64 bytes.  1 x 3072 x 3072 in 16 columns 4.6 us (32: 5.8, 64: 8.6, tiles of 64: 11), 8 x 12288 x 4096 in 64 columns 13.2 us (16: 15.0)
+  // Few rows: the time of loads of 16 rows by 64 bytes.  1 x 3072 x 3072 in 16 columns 4.6 us (32: 5.9, 64: 8.7, tiles of 64: 7.0), 1 x 8192 x 3072 gated in 32 columns 10.4 us
+  // (tiles of 64: 11.8), 8 x 12288 x 4096 in 64 columns 13.5 us (16: 15.0, tiles of 64: 11.4)
   for (int rows = 16; rows <= 32; rows *= 2)
     for (int columns = eight ? 128 : 16; columns <= (eight ? 128 : gated ? 32 : 64); columns *= 2) {
       if ((rows == 32 && (eight || p.M <= 16)) || (eight && gated)) continue;
@@ -723,23 +735,27 @@ MatmulPlan matmul8_plan(const svdc_matmul8& p) {
       const double loads = columns / 16 * (gated ? 2 : 1) + std::min<int64_t>(p.M, rows) / 16.0;
       consider({rows, columns, 1}, tiles, 2.5 + up(tiles, units) * up(blocks, 8) * (0.15 + 0.46 * loads) * (exact ? 1.3 : 1.0));
     }
-  // Tiles of 64: 0.37 us a block of latency, until the rounds of tiles take longer.  256 x 3072 x 3072 into float32 12.5 us (tiles of 128 in two parts: 20.7), 2000 x 1024 x 1024 6.0 us (128: 7.7)
+  // Tiles of 64: 0.37 us a block of latency, 0.24 with four stages, until the rounds of tiles take longer.  256 x 3072 x 3072 into float32 12.5 us (tiles of 128 in two
+  // parts: 20), into bfloat16 8.9 us (13.7); 2000 x 1024 x 1024 6.0 us (128: 7.7)
   const double tiles64 = up((double)p.M, 64) * up(p.N, eight ? 128 : 64), rounds64 = up(tiles64, units);
+  const int wide64 = (eight ? 2 : 1) * (gated ? 2 : 1);       // tiles of 64 by 64 wide64
   const double rate64 = (exact ? 0.28 : eight ? 0.31 : 0.175) * (gated ? 1.7 : 1.0);
-  consider({64, 64, 1}, tiles64, 2.5 + blocks * std::max(exact || eight || gated ? 0.42 : 0.37, rate64 * rounds64) + rounds64);
-  // Tiles of 128: 2000 x 3072 x 3072 25.6 us (64: 33, 256: 33.5).  In parts: 1160 x 320 x 11072 in eight 20.9 us (whole: 41)
-  const double rate128 = exact ? 0.75 : 0.42;
+  const double latency64 = can_be_deep(1, wide64, exact) && deep(tiles64, blocks, 1, wide64) ? 0.24 : exact || eight || gated ? 0.42 : 0.37;
+  consider({64, 64, 1}, tiles64, 2.5 + blocks * std::max(latency64, rate64 * rounds64) + rounds64);
+  // Tiles of 128: 2000 x 3072 x 3072 23.7 us (64: 32, 256: 32.6), 1000 x 3072 x 3072 15.3 us (64: 17.4).  In parts: 1160 x 320 x 11072 in eight 20.4 us (whole: 35)
   for (int splits = 1; splits <= 16; splits *= 2) {
     if (parts_of(blocks, splits) != splits) continue;
+    const int part = blocks_of_part(blocks, splits), wide128 = splits == 1 && gated && eight ? 4 : 2;
+    const double tiles = up((double)p.M, 128) * (splits > 1 ? up(wide_of(p), 128) : up(p.N, gated && !eight ? 64 : 128)) * splits;
+    const double rate128 = exact ? 0.75 : can_be_deep(2, wide128, false) && deep(tiles, part, 2, wide128) ? 0.38 : 0.42;
     if (splits == 1) {
-      const double tiles = up((double)p.M, 128) * up(p.N, gated && !eight ? 64 : 128);
       consider({128, 128, 1}, tiles, 3 + up(tiles, units) * (blocks * rate128 * (gated && eight ? 2 : 1) + 2));
     } else {
-      const double tiles = up((double)p.M, 128) * up(wide_of(p), 128) * splits, sums = (double)splits * p.M * wide_of(p);
-      consider({128, 128, splits}, tiles, 8 + up(tiles, units) * (((blocks + splits - 1) / splits + 3) / 4 * 4 * rate128 + 3) + sums * 8 / 4e6);
+      const double sums = (double)splits * p.M * wide_of(p);
+      consider({128, 128, splits}, tiles, 8 + up(tiles, units) * (part * rate128 + 3) + sums * 8 / 4e6);
     }
   }
-  // Tiles of 256: 4608 x 3072 x 3072 42.3 us (128: 51.5)
+  // Tiles of 256: 4608 x 3072 x 3072 40.4 us (128: 50)
   if (!exact) {
     const double tiles = up((double)p.M, 256) * up(p.N, gated ? 128 : 256);
     consider({256, 256, 1}, tiles, 4 + up(tiles, units) * (blocks * 1.25 + 9));
@@ -751,7 +767,13 @@ template <int TM, int TN, int ACT, int ES, bool EXACT>
 void launch_tiles(const MatmulArgs& a, hipStream_t st) {
   const int columns = ACT == SVDC_ACT_SWIGLU ? 32 * TN : 64 * TN;
   const int64_t tiles = (a.M + 64 * TM - 1) / (64 * TM) * ((a.N + columns - 1) / columns);
-  matmul8_tile_kernel<TM, TN, ACT, ES, EXACT><<<dim3((unsigned)tiles, a.splits), 256, 0, st>>>(a);
+  const dim3 grid((unsigned)tiles, a.splits);
+  if constexpr (can_be_deep(TM, TN, EXACT))
+    if (deep((double)tiles * a.splits, blocks_of_part(q8_blocks(a.K), a.splits), TM, TN)) {
+      matmul8_tile_kernel<TM, TN, ACT, ES, EXACT, 4><<<grid, 256, 0, st>>>(a);
+      return;
+    }
+  matmul8_tile_kernel<TM, TN, ACT, ES, EXACT, 2><<<grid, 256, 0, st>>>(a);
 }
 
 // Tiles of 64 T rows by 64 T columns.  Gated rows come in pairs of 32, and results in 8 bits need a whole block of columns: wider tiles of W where T is small.

@@ -217,6 +217,14 @@ def test_rms_norm8(rows, D, pad, offset, dtype, dtype_f):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,dtype_f", [(torch.bfloat16, torch.bfloat16), (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("rows,D", [(8195, 1000), (8195, 1101), (8193, 2040), (8194, 2501), (8195, 3001), (8195, 3100), (1030, 1025)])
+def test_rms_norm8_many_rows(rows, D, dtype, dtype_f):
+    """A row each for a wave or a workgroup of a full grid, and several rows for each of a small one."""
+    test_rms_norm8(rows, D, 3, 1, dtype, dtype_f)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,D", [(5, 3072), (2000, 1000)])
 def test_rms_norm8_outputs_on_their_own(rows, D):
     """Without F, gain, H; only Y; only Q; in place of X and of F: the same bits as with everything."""
@@ -603,3 +611,14 @@ WAYS = {
 @pytest.mark.parametrize("dtype,act,M,N,K", [(d, a, *s) for d, by in WAYS.items() for a, sizes in by.items() for s in sizes])
 def test_matmul8_every_way(dtype, act, M, N, K):
     check_product(M, N, K, dtype, act, with_bias=N % 2 == 1, seed=N, planted=M % 2 == 0, ldo_pad=5 if M % 3 == 0 else 0)
+
+
+# Few tiles and more than 8 blocks of columns: four blocks in flight instead of two.  9 to 13 blocks, so that every remainder of four ends the sums; tiles of 64, of 128, and
+# of 128 in parts.
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,act", [(torch.bfloat16, "none"), (torch.bfloat16, "gelu"), (torch.bfloat16, "swiglu"), (torch.float8_e4m3fn, "none"),
+                                       (torch.float8_e4m3fn, "gelu"), (torch.float8_e4m3fn, "swiglu")])
+@pytest.mark.parametrize("M,N,K", [(200, 1500, 1100), (130, 1031, 1157), (250, 1300, 1300), (190, 1411, 1537), (200, 1500, 1600), (1000, 3000, 1100), (1000, 1501, 1250),
+                                   (900, 2900, 1408), (1001, 3001, 1500), (255, 1100, 12000), (100, 8000, 6100)])
+def test_matmul8_few_tiles_of_long_sums(M, N, K, dtype, act):
+    check_product(M, N, K, dtype, act, with_bias=N % 2 == 1, seed=K, planted=M % 2 == 0, ldo_pad=3 if M % 3 == 0 else 0)
