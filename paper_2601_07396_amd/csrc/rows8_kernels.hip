@@ -2,7 +2,9 @@
 // (svdcache_quantize8).
 //
 // Both stream rows once: a lane holds 8 consecutive columns, so the 16 lanes of a DPP row hold the 128 columns that share a
-// scale, and the maximum over them is four register moves.  Neither reuses anything but the gain.
+// scale, and the maximum over them is four register moves.  Neither reuses anything but the gain.  Both are bound by memory (a copy of 1 GiB reaches 5.5 TB/s):
+//     norm      4608 x 3072 bfloat16 (99 MB) 16.4 us, 6.0 TB/s; 119056 x 3072 float32 with bfloat16 features (4.0 GB) 724 us, 5.6 TB/s; one row 3.0 us, a launch
+//     quantise  4608 x 3072 bfloat16 (42 MB) 8.3 us, 5.1 TB/s; 12288 x 3072 in blocks (113 MB) 24.0 us, 4.7 TB/s
 #include <algorithm>
 
 #include "eight_bit.h"
@@ -293,14 +295,18 @@ void norm_rows(const NormArgs& a, int chunks, unsigned grid, hipStream_t st) {
   }
 }
 
-// A wave a row up to 3072 columns, if that occupies the card; a workgroup of four waves up to 12288; longer rows do not fit in registers.
+// A wave a row where there are many rows of few columns (4608 x 1024 bfloat16 7.7 us, with four waves 8.6) or very many rows (119056 x 3072 float32 726 us, with four waves 751);
+// else a workgroup of four waves up to 12288 columns (4608 x 3072 bfloat16 17.8 us, with a wave 20.8; one row 3.0, with a wave 4.0); longer rows do not fit in registers.
+// Of middling numbers of rows a workgroup takes several, and keeps the gain (4608 rows 17.8 us, a row each 19.3); of many it takes one: they then stream through memory in
+// order (119056 rows 726 us, eight workgroups a unit 766).
 template <typename TX, typename TF>
 void norm(const NormArgs& a, hipStream_t st) {
   const int64_t units = num_compute_units();
-  if (a.D <= 6 * 512 && a.rows >= 4 * units)
-    norm_rows<TX, TF, 1>(a, (a.D + 511) / 512, (unsigned)std::min((a.rows + 3) / 4, 8 * units), st);
+  const bool many = a.rows >= 32 * units;
+  if (a.rows >= 4 * units && (a.D <= 1024 || (a.D <= 6 * 512 && many)))
+    norm_rows<TX, TF, 1>(a, (a.D + 511) / 512, grid_of((a.rows + 3) / 4), st);
   else if (a.D <= 6 * 2048)
-    norm_rows<TX, TF, 4>(a, (a.D + 2047) / 2048, (unsigned)std::min(a.rows, 8 * units), st);
+    norm_rows<TX, TF, 4>(a, (a.D + 2047) / 2048, grid_of(many ? a.rows : std::min(a.rows, 6 * units)), st);
   else
     rms_norm8_long_kernel<TX, TF, 16><<<grid_of(a.rows), 16 * kWave, 0, st>>>(a);
 }
