@@ -267,10 +267,11 @@ __global__ __launch_bounds__(kShareWaves* kWave) void matmul8_shared_kernel(Matm
 // lie in two register sets, one read from LDS while the other is multiplied.  Rows of 128 bytes are eight 16-byte slots; slot s of row r holds columns
 // 16 (s ^ swizzle(r)): eight consecutive rows and the rows of one parity of sixteen have different slots of a column, so that reads meet no bank twice.
 //
-// What bounds it.  Tiles of 256, one workgroup on a compute unit: the matrix cores and their clock, which the card lowers under this load to 1.76 GHz: 4608 x 3072 x 12288 147 us,
-// 2370 TFLOP/s, matrix cores 83 % busy; and the tile's ends, when they stand still (first loads 3.5 us, sums to results 4 us, GELU 3.5 us, stores 2 us in 8 bits and 8 us in bfloat16 a tile, all units at once): 18432 x 12288 x
-// 3072 with GELU into 8 bits 588 us, 2370 TFLOP/s, 63 % busy.  Tiles of 64 and 128: the latency of loads for each block, less of it with four stages (where they pay: see
-// deep() below).  Results in float32: widening, 64 conversions a block and wave; 256 x 3072 x 3072 12.2 us, 22 % busy.
+// What bounds it.  Tiles of 256, one workgroup on a compute unit: the matrix cores and their clock, which the card lowers under this load to 1.76 GHz: 4608 x 3072 x
+// 12288 147 us, 2370 TFLOP/s, matrix cores 83 % busy; and the tile's ends, when they stand still (first loads 3.5 us, sums to results 4 us, GELU 3.5 us, stores 2 us in
+// 8 bits and 8 us in bfloat16, all units at once): 18432 x 12288 x 3072 with GELU into 8 bits 590 us, 2360 TFLOP/s, 63 % busy.  Tiles of 64 and 128: the latency of loads
+// for each block, less of it with four stages (where they pay: see deep() below).  Results in float32: widening, 64 conversions a block and wave; 256 x 3072 x 3072
+// 12.2 us, 22 % busy.
 __device__ __forceinline__ int swizzle(int row) { return (row & 7) ^ (row >> 3 & 1); }
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));

@@ -78,7 +78,7 @@ __global__ void copy_status_kernel(const int32_t* __restrict__ src, int32_t* __r
 
 extern "C" {
 
-int32_t svdcache_version(void) { return 300; }   // 0.3.0: fit status words, svdcache_workspace_bytes
+int32_t svdcache_version(void) { return 400; }   // 0.4.0: operators of a block in 8 bits
 
 const char* svdcache_strerror(int32_t status) {
   switch (status) {
