@@ -8,7 +8,9 @@
 //
 // The instruction adds the products of 8 consecutive bytes with 13 bits below the largest of them (measured: smaller bits are cut off), then those sums in
 // float32.  That is about 4e-5 of a result: nothing beside the rounding of a result to bfloat16 or e4m3, but not float32.  Results in float32 are made with
-// bfloat16 instructions, at half the rate: e4m3 values times powers of two are bfloat16 values exactly, and those products are summed with 24 bits.
+// bfloat16 instructions, at half the rate: e4m3 values are bfloat16 values exactly, and their products are summed with 24 bits.  With their scales they are bfloat16 values
+// too, but for scales near the ends of their range (448 * 2^126 is above the largest bfloat16, 2^-9 * 2^-126 below the smallest): there a block's sums are made without
+// scales and enter the others times 2^(exponent of A + exponent of W), which is in range wherever the result is.
 #include <algorithm>
 
 #include "eight_bit.h"
@@ -38,22 +40,39 @@ __device__ __forceinline__ f32x4 mfma8(const i32x8& w, const i32x8& a, const f32
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, sw, 0, sa);
 }
 
-// 8 e4m3 values times 2^(byte - 127) as bfloat16, exactly
-__device__ __forceinline__ bf16x8 widen8(int lo, int hi, int byte) {
-  const float s = __uint_as_float((uint32_t)byte << 23);
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true),
-               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true);
+// 8 e4m3 values times `scale`, a power of two, as bfloat16: exactly for scales with in_range
+__device__ __forceinline__ bf16x8 widen8(int lo, int hi, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true),
+               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+__device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+// 2^-9 * scale is a normal number (byte >= 10) and 448 * scale a finite one (byte <= 246)
+__device__ __forceinline__ bool in_range(int byte) { return (uint32_t)byte - 10 <= 236; }
 
-// 128 columns of 16 rows of W and of A; EXACT: with float32 sums
-template <bool EXACT>
-__device__ __forceinline__ f32x4 product(const i32x8& w, const i32x8& a, f32x4 c, int sw, int sa) {
-  if (!EXACT) return mfma8(w, a, c, sw, sa);
+// Exponents of the scales of the sums of a column: `a` of its row of A, and of rows of W that lie in one block of 128 up to row `edge` (one number for all lanes), in the
+// next from there on.  All as bytes, of W's a lane's for its own row.
+struct Exponents {
+  int below, above, edge;
+  __device__ __forceinline__ Exponents(int w, int a) : below(w + a - 254), above(0), edge(INT32_MAX) {}
+  __device__ __forceinline__ Exponents(int w, int a, int edge, int last)
+      : below(__builtin_amdgcn_readlane(w, 0) + a - 254), above(__builtin_amdgcn_readlane(w, last) + a - 254), edge(edge) {}
+  __device__ __forceinline__ int operator[](int row) const { return row < edge ? below : above; }
+};
+
+// c += t * 2^exponent: sums of a block of columns, of which the e-th lies in row row_of(e) of the tile
+template <typename Sums, typename Row>
+__device__ __forceinline__ void add_scaled(Sums& c, const Sums& t, const Exponents& exponent, Row&& row_of) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2 * i], w[2 * i + 1], sw), widen8(a[2 * i], a[2 * i + 1], sa), c, 0, 0, 0);
-  return c;
+  for (int e = 0; e < (int)(sizeof(Sums) / sizeof(float)); ++e) c[e] += __builtin_amdgcn_ldexpf(t[e], exponent[row_of(e)]);
+}
+
+// 128 columns of 16 rows of W and of A, without scales and with float32 sums
+__device__ __forceinline__ f32x4 widened(const i32x8& w, const i32x8& a) {
+  f32x4 t = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2 * i], w[2 * i + 1], 1.f), widen8(a[2 * i], a[2 * i + 1], 1.f), t, 0, 0, 0);
+  return t;
 }
 
 // x / (1 + exp(-t)), with the hardware's power of two and reciprocal (one step of the last place each): half the instructions of a division
@@ -143,6 +162,8 @@ __device__ __forceinline__ void shared_sums(const MatmulArgs& a) {
     }
   };
   f32x4 c[NW][TM] = {};
+  // rows of tile i of what the gates gate that lie before the next block of 128 rows
+  const auto edge = [&](int i) { return kScaleBlock - (a.N + n0 + 16 * i) % kScaleBlock; };
   const auto multiply = [&](int b, const Operands& o) {
     int s[SCALES];                         // the block's byte, lowest
 #pragma unroll
@@ -155,7 +176,14 @@ __device__ __forceinline__ void shared_sums(const MatmulArgs& a) {
 #pragma unroll
     for (int i = 0; i < NW; ++i)
 #pragma unroll
-      for (int j = 0; j < TM; ++j) c[i][j] = product<EXACT>(o.x[TM + i], o.x[j], c[i][j], s[i < TN ? TM : TM + 1 + i - TN], s[j]);
+      for (int j = 0; j < TM; ++j) {
+        const int sw = s[i < TN ? TM : TM + 1 + i - TN];
+        if (!EXACT) {
+          c[i][j] = mfma8(o.x[TM + i], o.x[j], c[i][j], sw, s[j]);
+        } else {
+          add_scaled(c[i][j], widened(o.x[TM + i], o.x[j]), i < TN ? Exponents(sw, s[j]) : Exponents(sw, s[j], edge(i - TN), 15), [&](int e) { return 4 * g + e; });
+        }
+      }
   };
   Operands o[DEPTH];
   int b = wave;
@@ -276,15 +304,10 @@ __device__ __forceinline__ int swizzle(int row) { return (row & 7) ^ (row >> 3 &
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-template <bool EXACT>
-__device__ __forceinline__ void product32(f32x16& c, const i32x8& w, const i32x8& a, int sw, int sa) {
-  if (!EXACT) {
-    c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, a, c, 0, 0, 0, sw, 0, sa);
-  } else {
+// c += the sums of 64 columns of 32 rows of W and of A, in float32, from operands with their scales
+__device__ __forceinline__ void widened32(f32x16& c, const i32x8& w, const i32x8& a, float sw, float sa) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(w[2 * i], w[2 * i + 1], sw & 255), widen8(a[2 * i], a[2 * i + 1], sa & 255), c, 0, 0, 0);
-  }
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(w[2 * i], w[2 * i + 1], sw), widen8(a[2 * i], a[2 * i + 1], sa), c, 0, 0, 0);
 }
 
 // An instruction is issued here and not where the compiler would move it, with its sums in accumulation registers
@@ -569,13 +592,18 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) read(x[0], stages[0], p, 0);
 
+  int scale_bits = 255;                  // 0 for a block whose scales leave the range of bfloat16: it enters with scales of 0 here, and with its own behind the others
+  bool left_out = false;                 // one answer for the wave
   const auto multiply = [&](const i32x8* y, auto&& between) {
 #pragma unroll
     for (int i = 0; i < TN; ++i)
 #pragma unroll
       for (int j = 0; j < TM; ++j) {
         between(i * TM + j);
-        product32<EXACT>(c[i][j], y[i], y[TN + j], sc[i], sc[TN + j]);
+        if (EXACT)
+          widened32(c[i][j], y[i], y[TN + j], scale_of(sc[i] & scale_bits), scale_of(sc[TN + j] & scale_bits));
+        else
+          c[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(y[i], y[TN + j], c[i][j], 0, 0, 0, sc[i], 0, sc[TN + j]);
         hold(c[i][j]);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -583,6 +611,13 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
   // Block b lies in `now` with its first half in x[0].  Once all waves have read its second half, block b + STAGES is loaded there; beyond the last one the
   // loads are out of bounds and fetch nothing.
   const auto block = [&](int b, uint8_t* now, uint8_t* then) {
+    if (EXACT) {
+      bool good = true;
+#pragma unroll
+      for (int t = 0; t < TN + TM; ++t) good = good && in_range(sc[t] & 255);
+      scale_bits = __builtin_amdgcn_ballot_w64(!good) == 0 ? 255 : 0;
+      left_out = left_out || scale_bits == 0;
+    }
     const int more = b + STAGES < blocks ? -1 : 0;
     const auto A2 = bounded(a.A + m0 * Kp, a_bytes & more), W2 = bounded(a.W + n0 * Kp, w_bytes & more), U2 = bounded(a.W + u_first * Kp, w_bytes & more);
     multiply(x[0], [&](int t) {
@@ -620,6 +655,41 @@ __device__ __forceinline__ void tile_of_product(MatmulArgs a) {
     if (b + 1 < blocks) {
       block(b + 1, stages[1], stages[2]);
       if (b + 2 < blocks) block(b + 2, stages[2], stages[3]);
+    }
+  }
+  if constexpr (EXACT) {
+    if (left_out) {
+      // the blocks left out, each without scales and then times them, straight from memory: rare, so short rather than fast
+      const auto edge = [&](int i) { return kScaleBlock - (a.N + n0 + wn * 16 * TN + 32 * (i - TN / 2)) % kScaleBlock; };   // as in the few rows' kernel
+      const auto operand = [&](const uint8_t* row) {
+        const u32x4 lo = reinterpret_cast<const u32x4*>(row)[0], hi = reinterpret_cast<const u32x4*>(row)[1];
+        return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+      };
+      for (int d = 0; d < blocks; ++d) {
+        int s[TN + TM];
+        bool good = true;
+#pragma unroll
+        for (int t = 0; t < TN + TM; ++t) {
+          s[t] = t < TN ? a.Ws[scale_row[t] + d] : a.As[m0 * ss + scale_row[t] + d];
+          good = good && in_range(s[t]);
+        }
+        if (__builtin_amdgcn_ballot_w64(!good) == 0) continue;
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int j = 0; j < TM; ++j) {
+            f32x16 t = {};
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const int64_t col = d * 128 + half * 64 + h * 32;
+              widened32(t, operand(a.W + w_row(wn * 32 * TN + i * 32 + r) * Kp + col), operand(a.A + a_row(wm * 32 * TM + j * 32 + r) * Kp + col), 1.f, 1.f);
+            }
+            add_scaled(c[i][j], t, GATED && i >= TN / 2 ? Exponents(s[i], s[TN + j], edge(i), 31) : Exponents(s[i], s[TN + j]),
+                       [&](int e) { return e / 4 * 8 + 4 * h + e % 4; });
+            hold(c[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+      }
     }
   }
   asm volatile("s_waitcnt lgkmcnt(0) vmcnt(0)\n\ts_barrier" ::: "memory");
