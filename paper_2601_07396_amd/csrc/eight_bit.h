@@ -1,18 +1,12 @@
 // Values in e4m3 with scales that are powers of two: what the kernels that make them and the ones that read them share.
 #pragma once
+#include "eight_bit_sizes.h"
 #include "svdc_device.h"
 
 namespace svdc {
 
 // 16 bytes aligned to the smallest element: global memory takes wide accesses at any such address
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-
-constexpr int kScaleBlock = 128;   // columns (and, for weights, rows) that share a scale
-
-__host__ __device__ inline int q8_blocks(int D) { return (D + kScaleBlock - 1) / kScaleBlock; }
-__host__ __device__ inline int64_t q8_row_bytes(int D) { return (int64_t)q8_blocks(D) * kScaleBlock; }
-// a reader takes the scales of four blocks as one word
-__host__ __device__ inline int q8_scale_row_bytes(int D) { return (q8_blocks(D) + 3) / 4 * 4; }
 
 // The scale of a block as its stored byte: 2^(byte - 127) for the least power of two with amax <= 448 * 2^e, e in -126 .. 126.
 // With amax = 1.m * 2^(x - 127) and 448 = 1.75 * 2^8 that is e = x - 135, and one more where 1.m > 1.75.  An infinity counts as the

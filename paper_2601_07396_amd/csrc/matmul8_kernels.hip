@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "eight_bit.h"
+#include "matmul8_plan.h"
 #include "svdc_internal.h"
 
 namespace svdc {
@@ -30,11 +31,6 @@ struct MatmulArgs {
   int64_t M, ldo;
   int N, K, dtype, act, splits;
 };
-
-// blocks of each of `splits` parts of the columns of A and W: a multiple of four, as scales are read four at a time; the last part may have fewer
-__host__ __device__ __forceinline__ int blocks_of_part(int blocks, int splits) {
-  return splits == 1 ? blocks : ((blocks + splits - 1) / splits + 3) / 4 * 4;
-}
 
 __device__ __forceinline__ f32x4 mfma8(const i32x8& w, const i32x8& a, const f32x4& c, int sw, int sa) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, sw, 0, sa);
@@ -298,7 +294,7 @@ __global__ __launch_bounds__(kShareWaves* kWave) void matmul8_shared_kernel(Matm
 // What bounds it.  Tiles of 256, one workgroup on a compute unit: the matrix cores and their clock, which the card lowers under this load to 1.76 GHz: 4608 x 3072 x
 // 12288 147 us, 2370 TFLOP/s, matrix cores 83 % busy; and the tile's ends, when they stand still (first loads 3.5 us, sums to results 4 us, GELU 3.5 us, stores 2 us in
 // 8 bits and 8 us in bfloat16, all units at once): 18432 x 12288 x 3072 with GELU into 8 bits 590 us, 2360 TFLOP/s, 63 % busy.  Tiles of 64 and 128: the latency of loads
-// for each block, less of it with four stages (where they pay: see deep() below).  Results in float32: widening, 64 conversions a block and wave; 256 x 3072 x 3072
+// for each block, less of it with four stages (where they pay: see deep() in matmul8_plan.h).  Results in float32: widening, 64 conversions a block and wave; 256 x 3072 x 3072
 // 12.2 us, 22 % busy.
 __device__ __forceinline__ int swizzle(int row) { return (row & 7) ^ (row >> 3 & 1); }
 
@@ -761,112 +757,41 @@ __global__ __launch_bounds__(256) void matmul8_finish_kernel(MatmulArgs a, const
   }
 }
 
-// ---- which of them ---------------------------------------------------------------------------------------------------
-
-// How a product is made.  rows 16 or 32: workgroups of that many rows by `columns` (16, 32, 64; 16 by 128 for results in 8 bits) whose waves share the blocks;
-// rows 64, 128 or 256: tiles of that size through LDS, `splits` parts of the columns of A and W (of 128 only).
-struct MatmulPlan {
-  int rows, columns, splits;
-};
-
-constexpr double kMaxTiles = 1 << 22;         // workgroups of a launch, far below what its 32-bit counts hold
-
-int wide_of(const svdc_matmul8& p) { return p.act == SVDC_ACT_SWIGLU ? 2 * p.N : p.N; }
-
-// parts of the columns of A and W of which none is empty
-int parts_of(int blocks, int splits) { return (blocks + blocks_of_part(blocks, splits) - 1) / blocks_of_part(blocks, splits); }
-
-// Whether tiles of 64 TM by 64 TN with sums of `blocks` blocks have four stages in LDS instead of two: where all of them are at work at once all the same and the sums
-// are long enough.  256 x 3072 x 3072 into bfloat16, 192 tiles of 64: 8.9 us with four, 11.7 with two; 512 x 12288 x 3072, 1536 tiles: 35 and 27; 448 x 4096 x 1024:
-// 6.1 and 5.9.  With float32 sums a block takes its time from widening the operands (256 x 3072 x 3072 12.5 us with either): two.
-constexpr int kUnitLds = 160 << 10, kDeepLds = 128 << 10;
-constexpr int tile_lds(int TM, int TN, int stages) { return stages * 64 * (TM + TN) * 128; }
-constexpr bool can_be_deep(int TM, int TN, bool exact) { return !exact && tile_lds(TM, TN, 4) <= kDeepLds; }
-bool deep(double tiles, int blocks, int TM, int TN) { return blocks > 8 && tiles <= (double)num_compute_units() * (kUnitLds / tile_lds(TM, TN, 4)); }
-
-// The least of estimated times, in us: for each way what its rounds of workgroups (one on each compute unit; where several fit, they share it and
-// take as long) cost for a block of columns and for their ends.  Measured over some 40 products of 1 to 18432 rows, 100 to 18432 columns, K of 100 to 12288: the estimate is
-// within a quarter of the time, the way taken mostly within a twentieth and at most a sixth (32 x 4096 x 4096, gated) above the fastest way's.
-MatmulPlan matmul8_plan(const svdc_matmul8& p) {
-  const bool gated = p.act == SVDC_ACT_SWIGLU, exact = p.dtype == SVDC_F32, eight = p.dtype == SVDC_E4M3;
-  const double units = num_compute_units();
-  const int blocks = q8_blocks(p.K);
-  const auto up = [](double x, double y) { return (double)(int64_t)((x + y - 1) / y); };
-  MatmulPlan best{};
-  double least = 1e300;
-  const auto consider = [&](MatmulPlan plan, double tiles, double us) {
-    if (us < least && tiles <= kMaxTiles) least = us, best = plan;
-  };
-  // Few rows: the time of loads of 16 rows by 64 bytes.  1 x 3072 x 3072 in 16 columns 4.6 us (32: 5.9, 64: 8.7, tiles of 64: 7.0), 1 x 8192 x 3072 gated in 32 columns 10.4 us
-  // (tiles of 64: 11.8), 8 x 12288 x 4096 in 64 columns 13.5 us (16: 15.0, tiles of 64: 11.4)
-  for (int rows = 16; rows <= 32; rows *= 2)
-    for (int columns = eight ? 128 : 16; columns <= (eight ? 128 : gated ? 32 : 64); columns *= 2) {
-      if ((rows == 32 && (eight || p.M <= 16)) || (eight && gated)) continue;
-      const double tiles = up((double)p.M, rows) * up(p.N, columns);
-      const double loads = columns / 16 * (gated ? 2 : 1) + std::min<int64_t>(p.M, rows) / 16.0;
-      consider({rows, columns, 1}, tiles, 2.5 + up(tiles, units) * up(blocks, 8) * (0.15 + 0.46 * loads) * (exact ? 1.3 : 1.0));
-    }
-  // Tiles of 64: 0.37 us a block of latency, 0.24 with four stages, until the rounds of tiles take longer.  256 x 3072 x 3072 into float32 12.5 us (tiles of 128 in two
-  // parts: 20), into bfloat16 8.9 us (13.7); 2000 x 1024 x 1024 6.0 us (128: 7.7)
-  const double tiles64 = up((double)p.M, 64) * up(p.N, eight ? 128 : 64), rounds64 = up(tiles64, units);
-  const int wide64 = (eight ? 2 : 1) * (gated ? 2 : 1);       // tiles of 64 by 64 wide64
-  const double rate64 = (exact ? 0.28 : eight ? 0.31 : 0.175) * (gated ? 1.7 : 1.0);
-  const double latency64 = can_be_deep(1, wide64, exact) && deep(tiles64, blocks, 1, wide64) ? 0.24 : exact || eight || gated ? 0.42 : 0.37;
-  consider({64, 64, 1}, tiles64, 2.5 + blocks * std::max(latency64, rate64 * rounds64) + rounds64);
-  // Tiles of 128: 2000 x 3072 x 3072 23.7 us (64: 32, 256: 32.6), 1000 x 3072 x 3072 15.3 us (64: 17.4).  In parts: 1160 x 320 x 11072 in eight 20.4 us (whole: 35)
-  for (int splits = 1; splits <= 16; splits *= 2) {
-    if (parts_of(blocks, splits) != splits) continue;
-    const int part = blocks_of_part(blocks, splits), wide128 = splits == 1 && gated && eight ? 4 : 2;
-    const double tiles = up((double)p.M, 128) * (splits > 1 ? up(wide_of(p), 128) : up(p.N, gated && !eight ? 64 : 128)) * splits;
-    const double rate128 = exact ? 0.75 : can_be_deep(2, wide128, false) && deep(tiles, part, 2, wide128) ? 0.38 : 0.42;
-    if (splits == 1) {
-      consider({128, 128, 1}, tiles, 3 + up(tiles, units) * (blocks * rate128 * (gated && eight ? 2 : 1) + 2));
-    } else {
-      const double sums = (double)splits * p.M * wide_of(p);
-      consider({128, 128, splits}, tiles, 8 + up(tiles, units) * (part * rate128 + 3) + sums * 8 / 4e6);
-    }
-  }
-  // Tiles of 256: 4608 x 3072 x 3072 40.4 us (128: 50)
-  if (!exact) {
-    const double tiles = up((double)p.M, 256) * up(p.N, gated ? 128 : 256);
-    consider({256, 256, 1}, tiles, 4 + up(tiles, units) * (blocks * 1.25 + 9));
-  }
-  return best;
-}
+// ---- launches --------------------------------------------------------------------------------------------------------
 
 template <int TM, int TN, int ACT, int ES, bool EXACT>
-void launch_tiles(const MatmulArgs& a, hipStream_t st) {
+void launch_tiles(const MatmulArgs& a, int stages, hipStream_t st) {
   const int columns = ACT == SVDC_ACT_SWIGLU ? 32 * TN : 64 * TN;
   const int64_t tiles = (a.M + 64 * TM - 1) / (64 * TM) * ((a.N + columns - 1) / columns);
   const dim3 grid((unsigned)tiles, a.splits);
   if constexpr (can_be_deep(TM, TN, EXACT))
-    if (deep((double)tiles * a.splits, blocks_of_part(q8_blocks(a.K), a.splits), TM, TN)) {
+    if (stages == 4) {
       matmul8_tile_kernel<TM, TN, ACT, ES, EXACT, 4><<<grid, 256, 0, st>>>(a);
       return;
     }
   matmul8_tile_kernel<TM, TN, ACT, ES, EXACT, 2><<<grid, 256, 0, st>>>(a);
 }
 
-// Tiles of 64 T rows by 64 T columns.  Gated rows come in pairs of 32, and results in 8 bits need a whole block of columns: wider tiles of W where T is small.
+// Tiles of 64 T rows by 64 tile_width() rows of W
 template <int T, int ES>
-void launch_tiles(const MatmulArgs& a, hipStream_t st) {
-  constexpr int PLAIN = ES == 1 && T < 2 ? 2 : T, GATES = ES == 1 && T < 4 ? 4 : T < 2 ? 2 : T;
+void launch_tiles(const MatmulArgs& a, int stages, hipStream_t st) {
+  constexpr int PLAIN = tile_width(64 * T, false, ES == 1), GATES = tile_width(64 * T, true, ES == 1);
   if (a.act == SVDC_ACT_SWIGLU)
-    launch_tiles<T, GATES, SVDC_ACT_SWIGLU, ES, ES == 4>(a, st);
+    launch_tiles<T, GATES, SVDC_ACT_SWIGLU, ES, ES == 4>(a, stages, st);
   else if (a.act == SVDC_ACT_GELU)
-    launch_tiles<T, PLAIN, SVDC_ACT_GELU, ES, ES == 4>(a, st);
+    launch_tiles<T, PLAIN, SVDC_ACT_GELU, ES, ES == 4>(a, stages, st);
   else
-    launch_tiles<T, PLAIN, SVDC_ACT_NONE, ES, ES == 4>(a, st);
+    launch_tiles<T, PLAIN, SVDC_ACT_NONE, ES, ES == 4>(a, stages, st);
 }
 
 template <int T>
-void launch_tiles(const MatmulArgs& a, hipStream_t st) {
+void launch_tiles(const MatmulArgs& a, int stages, hipStream_t st) {
   if (a.dtype == SVDC_F32)
-    launch_tiles<T, 4>(a, st);
+    launch_tiles<T, 4>(a, stages, st);
   else if (a.dtype == SVDC_BF16)
-    launch_tiles<T, 2>(a, st);
+    launch_tiles<T, 2>(a, stages, st);
   else
-    launch_tiles<T, 1>(a, st);
+    launch_tiles<T, 1>(a, stages, st);
 }
 
 template <int TM, int TN, bool EXACT, bool GATED, bool EIGHT>
@@ -900,9 +825,9 @@ int32_t launch_planned(const MatmulPlan& plan, MatmulArgs a, void* workspace, hi
   if (plan.rows <= 32) {
     launch_shared(a, plan, st);
   } else if (plan.rows == 256) {
-    a.dtype == SVDC_BF16 ? launch_tiles<4, 2>(a, st) : launch_tiles<4, 1>(a, st);
+    a.dtype == SVDC_BF16 ? launch_tiles<4, 2>(a, plan.stages, st) : launch_tiles<4, 1>(a, plan.stages, st);
   } else if (plan.splits == 1) {
-    plan.rows == 64 ? launch_tiles<1>(a, st) : launch_tiles<2>(a, st);
+    plan.rows == 64 ? launch_tiles<1>(a, plan.stages, st) : launch_tiles<2>(a, plan.stages, st);
   } else {
     MatmulArgs part = a;                       // plain sums of all of W's rows
     part.N = a.act == SVDC_ACT_SWIGLU ? 2 * a.N : a.N;
@@ -910,7 +835,7 @@ int32_t launch_planned(const MatmulPlan& plan, MatmulArgs a, void* workspace, hi
     part.bias = nullptr;
     part.Out = workspace;
     part.ldo = part.N;
-    a.dtype == SVDC_F32 ? launch_tiles<2, 2, SVDC_ACT_NONE, 4, true>(part, st) : launch_tiles<2, 2, SVDC_ACT_NONE, 4, false>(part, st);
+    a.dtype == SVDC_F32 ? launch_tiles<2, 2, SVDC_ACT_NONE, 4, true>(part, plan.stages, st) : launch_tiles<2, 2, SVDC_ACT_NONE, 4, false>(part, plan.stages, st);
     if (hipGetLastError() != hipSuccess) return SVDC_E_HIP;
     const int64_t groups = (a.M * q8_blocks(a.N) + 15) / 16;
     matmul8_finish_kernel<<<(unsigned)std::min<int64_t>(groups, 1 << 20), 256, 0, st>>>(a, static_cast<const float*>(workspace));
@@ -921,7 +846,7 @@ int32_t launch_planned(const MatmulPlan& plan, MatmulArgs a, void* workspace, hi
 }  // namespace
 
 size_t matmul8_workspace_bytes(const svdc_matmul8& p) {
-  const MatmulPlan plan = matmul8_plan(p);
+  const MatmulPlan plan = matmul8_plan(p, num_compute_units());
   return plan.splits <= 1 ? 0 : (size_t)plan.splits * p.M * wide_of(p) * sizeof(float);
 }
 
@@ -929,7 +854,7 @@ int32_t launch_matmul8(const svdc_matmul8& p, const void* A, const void* As, con
                        void* workspace, hipStream_t st) {
   const MatmulArgs a{static_cast<const uint8_t*>(A), static_cast<const uint8_t*>(As), static_cast<const uint8_t*>(W), static_cast<const uint8_t*>(Ws),
                      bias, Out, static_cast<uint8_t*>(Os), p.M, p.ldo, p.N, p.K, p.dtype, p.act, 1};
-  const MatmulPlan plan = matmul8_plan(p);
+  const MatmulPlan plan = matmul8_plan(p, num_compute_units());
   if (plan.rows == 0) return SVDC_E_SHAPE;          // a result of more than 2^38 elements
   return launch_planned(plan, a, workspace, st);
 }
