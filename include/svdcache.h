@@ -406,8 +406,7 @@ size_t svdcache_matmul8_workspace_bytes(const svdc_matmul8* p);
  *   Out_scales    out  its scales for E4M3, else not read
  *   workspace     device scratch of svdcache_matmul8_workspace_bytes() bytes, 256-byte aligned, NULL where that is 0.  It belongs to the call until it
  *                 has completed on the stream: calls in flight on different streams need one each.
- * Results do not depend on anything but the arguments and the number of compute units (no atomics).  SVDC_E_SHAPE for results of more than 2^36
- * elements (2^38 in tiles of 256), which no device holds. */
+ * Results do not depend on anything but the arguments and the number of compute units (no atomics). */
 int32_t svdcache_matmul8(const svdc_matmul8* p, const void* A, const void* A_scales, const void* W, const void* W_scales,
                          const float* bias, void* Out, void* Out_scales, void* workspace, size_t workspace_bytes,
                          void* stream);

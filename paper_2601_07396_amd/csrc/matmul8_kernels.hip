@@ -824,10 +824,23 @@ int32_t launch_planned(const MatmulPlan& plan, MatmulArgs a, void* workspace, hi
   a.splits = plan.splits;
   if (plan.rows <= 32) {
     launch_shared(a, plan, st);
-  } else if (plan.rows == 256) {
-    a.dtype == SVDC_BF16 ? launch_tiles<4, 2>(a, plan.stages, st) : launch_tiles<4, 1>(a, plan.stages, st);
   } else if (plan.splits == 1) {
-    plan.rows == 64 ? launch_tiles<1>(a, plan.stages, st) : launch_tiles<2>(a, plan.stages, st);
+    const bool eight = a.dtype == SVDC_E4M3;
+    const int64_t most = rows_of_launch(plan, a.N, a.act == SVDC_ACT_SWIGLU, eight);
+    const int64_t out_row = eight ? q8_row_bytes(a.N) : a.ldo * (a.dtype == SVDC_F32 ? 4 : 2);
+    for (int64_t left = a.M; left > 0; left -= most) {
+      a.M = std::min(left, most);
+      if (plan.rows == 256)
+        a.dtype == SVDC_BF16 ? launch_tiles<4, 2>(a, plan.stages, st) : launch_tiles<4, 1>(a, plan.stages, st);
+      else
+        plan.rows == 64 ? launch_tiles<1>(a, plan.stages, st) : launch_tiles<2>(a, plan.stages, st);
+      if (hipGetLastError() != hipSuccess) return SVDC_E_HIP;
+      a.A += most * q8_row_bytes(a.K);
+      a.As += most * q8_scale_row_bytes(a.K);
+      a.Out = static_cast<uint8_t*>(a.Out) + most * out_row;
+      if (eight) a.Os += most * q8_scale_row_bytes(a.N);
+    }
+    return SVDC_OK;
   } else {
     MatmulArgs part = a;                       // plain sums of all of W's rows
     part.N = a.act == SVDC_ACT_SWIGLU ? 2 * a.N : a.N;
@@ -854,9 +867,7 @@ int32_t launch_matmul8(const svdc_matmul8& p, const void* A, const void* As, con
                        void* workspace, hipStream_t st) {
   const MatmulArgs a{static_cast<const uint8_t*>(A), static_cast<const uint8_t*>(As), static_cast<const uint8_t*>(W), static_cast<const uint8_t*>(Ws),
                      bias, Out, static_cast<uint8_t*>(Os), p.M, p.ldo, p.N, p.K, p.dtype, p.act, 1};
-  const MatmulPlan plan = matmul8_plan(p, num_compute_units());
-  if (plan.rows == 0) return SVDC_E_SHAPE;          // a result of more than 2^38 elements
-  return launch_planned(plan, a, workspace, st);
+  return launch_planned(matmul8_plan(p, num_compute_units()), a, workspace, st);
 }
 
 }  // namespace svdc

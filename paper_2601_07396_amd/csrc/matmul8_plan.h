@@ -22,7 +22,13 @@ struct MatmulPlan {
 // there are few rows.
 constexpr int tile_width(int rows, bool gated, bool eight) { return eight && gated ? 4 : (eight || gated) && rows < 128 ? 2 : rows / 64; }
 
-constexpr double kMaxTiles = 1 << 22;         // workgroups of a launch, far below what its 32-bit counts hold
+constexpr int kMaxTiles = 1 << 22;         // workgroups of a launch, far below what its 32-bit counts hold
+
+// Rows of A that one launch of tiles takes: all of them, but for results of very many rows.
+inline int64_t rows_of_launch(const MatmulPlan& plan, int N, bool gated, bool eight) {
+  const int columns = 64 * tile_width(plan.rows, gated, eight) / (gated ? 2 : 1);
+  return (int64_t)plan.rows * (kMaxTiles / ((N + columns - 1) / columns));
+}
 
 inline int wide_of(const svdc_matmul8& p) { return p.act == SVDC_ACT_SWIGLU ? 2 * p.N : p.N; }
 
@@ -49,8 +55,10 @@ inline MatmulPlan matmul8_plan(const svdc_matmul8& p, int cus) {
   const auto up = [](double x, double y) { return (double)(int64_t)((x + y - 1) / y); };
   MatmulPlan best{};
   double least = 1e300;
+  // one launch, but of the largest tiles of a type, which go on with the next rows in another
   const auto consider = [&](MatmulPlan plan, double tiles, double us) {
-    if (us < least && tiles <= kMaxTiles) least = us, best = plan;
+    const bool largest = plan.rows == (exact ? 128 : 256) && plan.splits == 1;
+    if (us < least && (tiles <= kMaxTiles || largest)) least = us, best = plan;
   };
   // Few rows: the time of loads of 16 rows by 64 bytes.  1 x 3072 x 3072 in 16 columns 4.6 us (32: 5.9, 64: 8.7, tiles of 64: 7.0), 1 x 8192 x 3072 gated in 32 columns 10.4 us
   // (tiles of 64: 11.8), 8 x 12288 x 4096 in 64 columns 13.5 us (16: 15.0, tiles of 64: 11.4)
