@@ -359,7 +359,8 @@ typedef struct {
  *   Y       out  [rows, D] dtype, y rounded; NULL if not wanted
  *   Q, scales  out  y in 8 bits (one scale per row and 128 columns); both NULL if not wanted
  * At least one of Y and Q is given; outputs overlap neither each other nor inputs but as said.  Pointers are aligned to their elements,
- * Q to 16 bytes, scales to 4.  A row of zeros gives zeros where eps > 0. */
+ * Q to 16 bytes, scales to 4.  A row of zeros gives zeros where eps > 0.  Squares and their sum are float32: a row whose sum of squares passes
+ * 3.4e38 gives zeros, and NaN where h is not finite. */
 int32_t svdcache_rms_norm8(const svdc_norm8* p, const void* X, const void* F, const float* gain, void* H, void* Y, void* Q,
                            void* scales, void* stream);
 

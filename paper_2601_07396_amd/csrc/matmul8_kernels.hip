@@ -98,7 +98,7 @@ __device__ __forceinline__ float finished(const MatmulArgs& a, int col, float z,
 //
 // What bounds it: the look-ups of lines by the loads.  A load of an operand takes 64 bytes of 16 rows, and lines are looked up one at a time: 54 MB of weights in this
 // pattern take 13.6 us alone, in 128 bytes of 8 rows 9.8 us, but the matrix instructions want 16 rows (instructions that waste half their work on the other pattern were no
-// faster).  1 x 18432 x 3072 into bfloat16 12.1 us (4.7 TB/s of weights; a read of as many bytes 8.7 us), 1 x 3072 x 3072 4.6 us.
+// faster).  1 x 18432 x 3072 into bfloat16 12.3 us (4.6 TB/s of weights; a read of as many bytes 8.7 us), 1 x 3072 x 3072 4.4 us.
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }   // a value that all lanes hold, as a scalar
 
@@ -293,10 +293,10 @@ __global__ __launch_bounds__(kShareWaves* kWave) void matmul8_shared_kernel(Matm
 // 16 (s ^ swizzle(r)): eight consecutive rows and the rows of one parity of sixteen have different slots of a column, so that reads meet no bank twice.
 //
 // What bounds it.  Tiles of 256, one workgroup on a compute unit: the matrix cores and their clock, which the card lowers under this load to 1.76 GHz: 4608 x 3072 x
-// 12288 147 us, 2370 TFLOP/s, matrix cores 83 % busy; and the tile's ends, when they stand still (first loads 3.5 us, sums to results 4 us, GELU 3.5 us, stores 2 us in
-// 8 bits and 8 us in bfloat16, all units at once): 18432 x 12288 x 3072 with GELU into 8 bits 590 us, 2360 TFLOP/s, 63 % busy.  Tiles of 64 and 128: the latency of loads
+// 12288 148 us, 2350 TFLOP/s, matrix cores 83 % busy; and the tile's ends, when they stand still (first loads 3.5 us, sums to results 4 us, GELU 3.5 us, stores 2 us in
+// 8 bits and 8 us in bfloat16, all units at once): 18432 x 12288 x 3072 with GELU into 8 bits 602 us, 2310 TFLOP/s, 63 % busy.  Tiles of 64 and 128: the latency of loads
 // for each block, less of it with four stages (where they pay: see deep() in matmul8_plan.h).  Results in float32: widening, 64 conversions a block and wave; 256 x 3072 x 3072
-// 12.2 us, 22 % busy.
+// 12.4 us, 22 % busy.
 __device__ __forceinline__ int swizzle(int row) { return (row & 7) ^ (row >> 3 & 1); }
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));

@@ -46,8 +46,10 @@ inline bool deep(double tiles, int blocks, int TM, int TN, bool exact, int units
 }
 
 // The least of estimated times, in us: for each way what its rounds of workgroups (one on each compute unit; where several fit, they share it and
-// take as long) cost for a block of columns and for their ends.  Measured over some 40 products of 1 to 18432 rows, 100 to 18432 columns, K of 100 to 12288: the estimate is
-// within a quarter of the time, the way taken mostly within a twentieth and at most a sixth (32 x 4096 x 4096, gated) above the fastest way's.
+// take as long) cost for a block of columns and for their ends.  Measured over 174 products (29 sizes of 1 to 18432 rows, 64 to 18432 columns, K of 100 to 12288; three types, with and
+// without gates): the estimate is within a quarter of the time for 163, the way taken within a twentieth of the fastest way's for 160 and within a sixth for 170.  The others are
+// 18432 x 12288 x 100 gated into 8 bits (1.27 times) and 200 x 300 x 8192 in 8 and 16 parts (1.28 to 2.9 times): where N is no multiple of 8, matmul8_finish_kernel
+// takes 0.55 us more for each part and sum (16 parts, gated, float32: N = 304 28 us, N = 300 47 us), which the estimate does not know.
 inline MatmulPlan matmul8_plan(const svdc_matmul8& p, int cus) {
   const bool gated = p.act == SVDC_ACT_SWIGLU, exact = p.dtype == SVDC_F32, eight = p.dtype == SVDC_E4M3;
   const double units = cus;
@@ -60,7 +62,7 @@ inline MatmulPlan matmul8_plan(const svdc_matmul8& p, int cus) {
     const bool largest = plan.rows == (exact ? 128 : 256) && plan.splits == 1;
     if (us < least && (tiles <= kMaxTiles || largest)) least = us, best = plan;
   };
-  // Few rows: the time of loads of 16 rows by 64 bytes.  1 x 3072 x 3072 in 16 columns 4.6 us (32: 5.9, 64: 8.7, tiles of 64: 7.0), 1 x 8192 x 3072 gated in 32 columns 10.4 us
+  // Few rows: the time of loads of 16 rows by 64 bytes.  1 x 3072 x 3072 in 16 columns 4.4 us (32: 5.9, 64: 8.7, tiles of 64: 7.0), 1 x 8192 x 3072 gated in 32 columns 10.4 us
   // (tiles of 64: 11.8), 8 x 12288 x 4096 in 64 columns 13.5 us (16: 15.0, tiles of 64: 11.4)
   for (int rows = 16; rows <= 32; rows *= 2)
     for (int columns = eight ? 128 : 16; columns <= (eight ? 128 : gated ? 32 : 64); columns *= 2) {

@@ -3,8 +3,8 @@
 //
 // Both stream rows once: a lane holds 8 consecutive columns, so the 16 lanes of a DPP row hold the 128 columns that share a
 // scale, and the maximum over them is four register moves.  Neither reuses anything but the gain.  Both are bound by memory (a copy of 1 GiB reaches 5.5 TB/s):
-//     norm      4608 x 3072 bfloat16 (99 MB) 16.4 us, 6.0 TB/s; 119056 x 3072 float32 with bfloat16 features (4.0 GB) 724 us, 5.6 TB/s; one row 3.0 us, a launch
-//     quantise  4608 x 3072 bfloat16 (42 MB) 8.3 us, 5.1 TB/s; 12288 x 3072 in blocks (113 MB) 24.0 us, 4.7 TB/s
+//     norm      4608 x 3072 bfloat16 (99 MB) 18.0 us, 5.5 TB/s; 119056 x 3072 float32 with bfloat16 features (4.0 GB) 729 us, 5.5 TB/s; one row 3.0 us, a launch
+//     quantise  4608 x 3072 bfloat16 (42 MB) 8.3 us, 5.1 TB/s; 12288 x 3072 in blocks (113 MB) 24.2 us, 4.7 TB/s
 #include <algorithm>
 
 #include "eight_bit.h"
@@ -177,7 +177,8 @@ __global__ __launch_bounds__(256) void rms_norm8_rows_kernel(NormArgs a) {
   }
 }
 
-// Longer rows: a workgroup of NW waves takes a row at a time and reads it twice, the second time out of the caches.
+// Longer rows: a workgroup of NW waves takes a row at a time and reads it twice, the second time out of the caches.  4608 x 16384 bfloat16 (528 MB without the second
+// read) 133 us, 4.0 TB/s; 300 x 20000 16.1 us; one row of 20000 6.8 us.
 template <typename TX, typename TF, int NW>
 __global__ __launch_bounds__(NW* kWave) void rms_norm8_long_kernel(NormArgs a) {
   __shared__ float part[NW];
