@@ -29,6 +29,9 @@
  *   svdcache_rms_norm8   the block's output enters the residual stream; its norm goes on in 8 bits (and / or plain)
  *   svdcache_quantize8   a matrix of activations or weights in 8 bits
  *   svdcache_matmul8     product of 8-bit activations and weights with bias, activation and an 8-bit result if wanted
+ *   svdcache_rotary_table / svdcache_norm_rotate / svdcache_attention
+ *                        from that product's queries, keys and values to the attention's output: angles of a rotation with several
+ *                        position axes, norm and rotation of each head, softmax(scale Q K^T) V
  *
  * General conventions
  *   - Every data pointer is a DEVICE pointer (HIP global memory) unless the
@@ -415,6 +418,100 @@ size_t svdcache_matmul8_workspace_bytes(const svdc_matmul8* p);
 int32_t svdcache_matmul8(const svdc_matmul8* p, const void* A, const void* A_scales, const void* W, const void* W_scales,
                          const float* bias, void* Out, void* Out_scales, void* workspace, size_t workspace_bytes,
                          void* stream);
+
+/* ---- Operators around a block's attention ----------------------------------------------------------------------------
+ *
+ * Tensors of heads are [batch, rows, heads, head_dim]: element (b, i, h, c) lies at b * seq + i * row + h * head + c.  So the column blocks of
+ * a product's result are read where they lie, and [batch, heads, rows, head_dim] is a matter of strides too. */
+typedef struct {
+  int64_t seq, row, head; /* strides in elements, 0 .. 2^40; row at most 2^22 */
+} svdc_heads;
+
+/* Most position axes of a rotation. */
+#define SVDC_MAX_AXES 4
+
+/* Which columns of a head make a pair: 2 j and 2 j + 1, or j and pairs + j. */
+typedef enum { SVDC_PAIRS_NEIGHBOURS = 0, SVDC_PAIRS_HALVES = 1 } svdc_pairs;
+
+/* Angles of a rotation with several position axes (time, height, width): axis a turns dims[a] / 2 pairs, those of axis 0 first. */
+typedef struct {
+  int64_t rows;                  /* 0 .. 2^31 - 1 */
+  int64_t ld;                    /* row stride of the positions in elements, at least axes, at most 2^24 */
+  int32_t axes;                  /* 1 .. SVDC_MAX_AXES */
+  int32_t whole;                 /* 0: positions are float32, 1: int32 */
+  int32_t dims[SVDC_MAX_AXES];   /* even, at least 2 for axes in use, 256 in all; not read for others */
+  double theta[SVDC_MAX_AXES];   /* > 0, finite; not read for axes not in use */
+} svdc_rotary;
+
+/* table[row][j] = (cos, sin) of pos[row][a] * theta[a]^(-2 i / dims[a]) with pair j the i-th of axis a.  Angles are made and reduced in 64 bits:
+ * positions as far as 2^31 lose nothing (an angle is off by at most 2^-51 of itself, cosine and sine by 2^-24 more).  A position that
+ * is not finite gives NaN.
+ *   pos    in   [rows, axes] float32 or int32
+ *   table  out  [rows, pairs, 2] float32, dense, 8-byte aligned, with pairs = sum of dims / 2 */
+int32_t svdcache_rotary_table(const svdc_rotary* p, const void* pos, float* table, void* stream);
+
+/* Norm and rotation of the heads of queries and keys. */
+typedef struct {
+  int64_t batch, rows;           /* batch * rows in 0 .. 2^31 - 1 */
+  int32_t heads, kv_heads;       /* of Q; of K and V.  1 .. 2^16 each */
+  int32_t head_dim;              /* 1 .. 256 */
+  int32_t dtype, dtype_out;      /* svdc_dtype of Q, K, V; of Qo, Ko, Vo: F32 or BF16 */
+  int32_t norm;                  /* 0: none (the gains are not read), 1: root mean square over a head */
+  int32_t pairs;                 /* 0 .. head_dim / 2 pairs are turned (0: the table is not read); columns from 2 pairs on are not */
+  int32_t layout;                /* svdc_pairs */
+  float eps;                     /* >= 0, finite */
+  int32_t reserved;              /* set to 0 */
+  int64_t table_seq;             /* from a sequence's table to the next one's in pairs; 0: all sequences share one.  0 .. 2^40 */
+  svdc_heads q, k, v, qo, ko, vo; /* strides of tensors that are NULL are not read */
+} svdc_norm_rotate;
+
+/* y = x * (1 / sqrt(mean_over_head(x^2) + eps)) * gain, then of each pair (a, b) of columns (a cos - b sin, a sin + b cos), in float32, rounded once.
+ *   Q, K          in   [batch, rows, heads / kv_heads, head_dim] dtype; either may be NULL together with its output
+ *   V             in   [batch, rows, kv_heads, head_dim] dtype or NULL: copied to Vo, in its type
+ *   gain_q, gain_k in  [head_dim] float32 or NULL: 1
+ *   table         in   [rows, pairs, 2] float32 (cos, sin) as svdcache_rotary_table writes it, 8-byte aligned, for each sequence or for all
+ *   Qo, Ko, Vo    out  as their inputs, of dtype_out; each may be the buffer of its own input if types and strides agree.  Outputs overlap
+ *                      neither each other nor inputs but so.  Rows and columns of a wider buffer that belong to no head stay.
+ * At least one of Q, K, V is given.  Pointers are aligned to their elements.  Squares and their sum are float32: a head whose sum of squares passes
+ * 3.4e38 gives zeros.  A head of zeros gives zeros where eps > 0. */
+int32_t svdcache_norm_rotate(const svdc_norm_rotate* p, const void* Q, const void* K, const void* V, const float* gain_q, const float* gain_k,
+                             const float* table, void* Qo, void* Ko, void* Vo, void* stream);
+
+/* One attention. */
+typedef struct {
+  int64_t batch;                 /* sequences, 0 .. 65535 */
+  int64_t q_rows, k_rows;        /* rows of a sequence, with spans the most that one has.  0 .. 2^31 - 1, batch times that as well */
+  int64_t q_total, k_total;      /* rows of Q and Out, of K and V, where spans say which of them a sequence has; else not read */
+  int32_t heads, kv_heads;       /* of Q and Out; of K and V: a divisor, each serves heads / kv_heads consecutive ones.  1 .. 2^16 */
+  int32_t head_dim;              /* 1 .. 256 */
+  int32_t dtype;                 /* svdc_dtype of all four: F32 or BF16 */
+  float scale;                   /* > 0, finite */
+  int32_t reserved;              /* set to 0 */
+  svdc_heads q, k, v, o;         /* seq is not read where spans are given */
+} svdc_attention;
+
+/* Bytes of device workspace that svdcache_attention needs: 0 where the rows of queries fill the card (and for an invalid one); few rows over
+ * many keys keep the results of parts of the keys there.  Spans and masks do not change it. */
+size_t svdcache_attention_workspace_bytes(const svdc_attention* p);
+
+/* Out = softmax(scale * Q K^T) V for each sequence and head; every query sees all keys of its sequence that the mask leaves.
+ *   Q         in   [batch, q_rows, heads, head_dim] dtype
+ *   K, V      in   [batch, k_rows, kv_heads, head_dim] dtype
+ *   q_span    in   [batch] pairs (first row, rows) of int32 on the device, or NULL.  Given, sequence b has these rows of Q and Out, as
+ *                  [q_total, heads, head_dim]: packed or padded sequences of any length from 0 on.  Other rows of Out stay as they were.
+ *                  Parts of a span outside 0 .. q_total - 1 or beyond q_rows rows are left out.  Spans of one call share no rows.
+ *   k_span    in   the same for K and V (k_rows, k_total), or NULL; spans may share rows
+ *   key_mask  in   a byte for each key, 0: left out; [batch, k_rows], with k_span [k_total]; or NULL.  What K and V hold for keys left out
+ *                  does not matter, whatever it is.
+ *   Out       out  as Q; overlaps no input.  A query without keys, or all of whose products are -infinity, gives zeros.
+ *   workspace      device scratch of svdcache_attention_workspace_bytes() bytes, 256-byte aligned, NULL where that is 0.  It belongs to the
+ *                  call until it has completed on the stream: calls in flight on different streams need one each.
+ * Pointers are aligned to their elements; rows and heads at multiples of 16 bytes of one another (pointers, strides and head_dim) are read faster.
+ * Products and sums, the softmax's maximum and sum are float32.  For bfloat16 the probabilities enter the second product rounded to
+ * bfloat16, which is as much off as rounding the result is; float32 uses float32 products throughout.  Results do not depend on anything but the
+ * arguments and the number of compute units (no atomics). */
+int32_t svdcache_attention(const svdc_attention* p, const void* Q, const void* K, const void* V, const int32_t* q_span, const int32_t* k_span,
+                           const uint8_t* key_mask, void* Out, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -22,6 +22,9 @@ from .binding import (
     svdcache_q8_scale_bytes, svdcache_rms_norm8, svdcache_quantize8, svdcache_matmul8_workspace_bytes,
     svdcache_matmul8, make_norm8, make_quant8, make_matmul8, alloc_q8, alloc_matmul8_workspace, rms_norm8, quantize8,
     matmul8,
+    Heads, Rotary, NormRotate, Attention, SVDC_MAX_AXES, SVDC_PAIRS_NEIGHBOURS, SVDC_PAIRS_HALVES, svdcache_rotary_table,
+    svdcache_norm_rotate, svdcache_attention_workspace_bytes, svdcache_attention, make_rotary, make_norm_rotate, make_attention,
+    alloc_attention_workspace, rotary_table, norm_rotate, attention,
 )
 
 __all__ = [
@@ -38,4 +41,7 @@ __all__ = [
     "svdcache_q8_bytes", "svdcache_q8_scale_bytes", "svdcache_rms_norm8", "svdcache_quantize8",
     "svdcache_matmul8_workspace_bytes", "svdcache_matmul8", "make_norm8", "make_quant8", "make_matmul8", "alloc_q8",
     "alloc_matmul8_workspace", "rms_norm8", "quantize8", "matmul8",
+    "Heads", "Rotary", "NormRotate", "Attention", "SVDC_MAX_AXES", "SVDC_PAIRS_NEIGHBOURS", "SVDC_PAIRS_HALVES",
+    "svdcache_rotary_table", "svdcache_norm_rotate", "svdcache_attention_workspace_bytes", "svdcache_attention", "make_rotary",
+    "make_norm_rotate", "make_attention", "alloc_attention_workspace", "rotary_table", "norm_rotate", "attention",
 ]

@@ -51,6 +51,35 @@ class Matmul8(C.Structure):
     _fields_ = [("M", C.c_int64), ("N", C.c_int32), ("K", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32), ("ldo", C.c_int64)]
 
 
+SVDC_MAX_AXES = 4
+
+
+class Heads(C.Structure):
+    """Mirror of svdc_heads."""
+    _fields_ = [("seq", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class Rotary(C.Structure):
+    """Mirror of svdc_rotary."""
+    _fields_ = [("rows", C.c_int64), ("ld", C.c_int64), ("axes", C.c_int32), ("whole", C.c_int32), ("dims", C.c_int32 * SVDC_MAX_AXES),
+                ("theta", C.c_double * SVDC_MAX_AXES)]
+
+
+class NormRotate(C.Structure):
+    """Mirror of svdc_norm_rotate."""
+    _fields_ = [("batch", C.c_int64), ("rows", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("dtype_out", C.c_int32), ("norm", C.c_int32), ("pairs", C.c_int32), ("layout", C.c_int32),
+                ("eps", C.c_float), ("reserved", C.c_int32), ("table_seq", C.c_int64), ("q", Heads), ("k", Heads), ("v", Heads),
+                ("qo", Heads), ("ko", Heads), ("vo", Heads)]
+
+
+class Attention(C.Structure):
+    """Mirror of svdc_attention."""
+    _fields_ = [("batch", C.c_int64), ("q_rows", C.c_int64), ("k_rows", C.c_int64), ("q_total", C.c_int64), ("k_total", C.c_int64),
+                ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float),
+                ("reserved", C.c_int32), ("q", Heads), ("k", Heads), ("v", Heads), ("o", Heads)]
+
+
 EXPORTS = {
     "svdcache_version": (C.c_int32, []),
     "svdcache_strerror": (C.c_char_p, [C.c_int32]),
@@ -95,6 +124,10 @@ EXPORTS = {
     "svdcache_quantize8": (C.c_int32, [C.POINTER(Quant8)] + [C.c_void_p] * 4),
     "svdcache_matmul8_workspace_bytes": (C.c_size_t, [C.POINTER(Matmul8)]),
     "svdcache_matmul8": (C.c_int32, [C.POINTER(Matmul8)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]),
+    "svdcache_rotary_table": (C.c_int32, [C.POINTER(Rotary)] + [C.c_void_p] * 3),
+    "svdcache_norm_rotate": (C.c_int32, [C.POINTER(NormRotate)] + [C.c_void_p] * 10),
+    "svdcache_attention_workspace_bytes": (C.c_size_t, [C.POINTER(Attention)]),
+    "svdcache_attention": (C.c_int32, [C.POINTER(Attention)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]),
 }
 
 _lib = None
@@ -139,7 +172,8 @@ def _load_fast_calls(lib):
         spec = importlib.util.spec_from_file_location("_fast_calls", path)
         fast = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(fast)
-        fast.bind({name: C.cast(getattr(lib, name), C.c_void_p).value for name in EXPORTS}, Shape, Norm8, Quant8, Matmul8)
+        fast.bind({name: C.cast(getattr(lib, name), C.c_void_p).value for name in EXPORTS}, Shape, Norm8, Quant8, Matmul8, Rotary,
+                  NormRotate, Attention)
     except Exception as e:
         warnings.warn(f"{path} does not load ({e}): step calls take about 4 us more host time each; "
                       "build it again with `python -m paper_2601_07396_amd.build`", RuntimeWarning, stacklevel=3)
@@ -594,6 +628,173 @@ def svdcache_matmul8(p: Matmul8, A, A_scales, W, W_scales, bias, Out, Out_scales
     _check(rc, "svdcache_matmul8")
 
 
+# ---- operators around a block's attention -------------------------------------------------------
+
+SVDC_PAIRS_NEIGHBOURS, SVDC_PAIRS_HALVES = 0, 1
+_PAIRS = {"neighbours": SVDC_PAIRS_NEIGHBOURS, "halves": SVDC_PAIRS_HALVES}
+
+
+def _on_current_device(*ts):
+    _need_gpu(*ts)
+    for t in ts:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise RuntimeError(f"svdcache: a tensor is on {t.device}, the call goes to the current device cuda:{torch.cuda.current_device()}")
+
+
+def _heads_of(name: str, t: torch.Tensor):
+    """(batch, rows, heads, head_dim, strides) of a tensor [batch, rows, heads, head_dim] or [rows, heads, head_dim]; strides of dimensions
+    that are not walked count as 0."""
+    if t.dim() not in (3, 4) or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: need [batch, rows, heads, head_dim] or [rows, heads, head_dim] with a contiguous last dimension, got {tuple(t.shape)} "
+                         f"with strides {t.stride()}")
+    shape = (1, *t.shape) if t.dim() == 3 else tuple(t.shape)
+    strides = (0, *t.stride()) if t.dim() == 3 else t.stride()
+    return (*shape, Heads(*(st if n > 1 else 0 for n, st in zip(shape[:3], strides))))
+
+
+def _check_heads(name: str, t, batch: int, rows: int, heads: int, head_dim: int, strides: Heads, dtype: int, out: bool = False):
+    """Refuses a tensor that is laid out otherwise than the descriptor says, and an output whose elements share memory."""
+    if t.dtype != _TORCH_OF[dtype]:
+        raise ValueError(f"{name}: dtype {t.dtype} is not {_TORCH_OF[dtype]}")
+    *shape, have = _heads_of(name, t)
+    if shape != [batch, rows, heads, head_dim]:
+        raise ValueError(f"{name}: {tuple(t.shape)} is not {batch} x {rows} rows of {heads} heads of {head_dim} columns")
+    for n, field in zip(shape, ("seq", "row", "head")):
+        if n > 1 and getattr(have, field) != getattr(strides, field):
+            raise ValueError(f"{name}: strides {t.stride()} are not those of the descriptor ({strides.seq}, {strides.row}, {strides.head})")
+    if out:
+        reach = head_dim
+        for st, n in sorted((getattr(have, field), n) for n, field in zip(shape, ("seq", "row", "head")) if n > 1):
+            if st < reach:
+                raise ValueError(f"{name}: elements of {tuple(t.shape)} with strides {t.stride()} share memory")
+            reach += (n - 1) * st
+
+
+def make_rotary(positions: torch.Tensor, dims, theta=10000.0) -> Rotary:
+    """Descriptor of the angles of positions [..., axes] (float32 or int32) with dims[a] columns of a head turned by axis a; theta: one number or
+    one for each axis."""
+    dims = [int(n) for n in dims]
+    theta = [float(x) for x in theta] if isinstance(theta, (list, tuple)) else [float(theta)] * len(dims)
+    if positions.dtype not in (torch.float32, torch.int32):
+        raise ValueError("positions must be float32 or int32")
+    rows, axes, ld = _row_stride("positions", positions)
+    if len(dims) != axes or len(theta) != axes or not 1 <= axes <= SVDC_MAX_AXES:
+        raise ValueError(f"positions with {axes} axes need as many dims and thetas, at most {SVDC_MAX_AXES}; got {len(dims)} and {len(theta)}")
+    return Rotary(rows, ld, axes, int(positions.dtype == torch.int32), (C.c_int32 * SVDC_MAX_AXES)(*dims), (C.c_double * SVDC_MAX_AXES)(*theta))
+
+
+def make_norm_rotate(Q=None, K=None, V=None, Qo=None, Ko=None, Vo=None, table=None, layout: str = "neighbours", norm: bool = True,
+                     eps: float = 1e-6) -> NormRotate:
+    """Descriptor of norm and rotation for tensors [batch, rows, heads, head_dim] (or without batch) laid out like these; V is copied.  table
+    [rows, pairs, 2], or [batch, rows, pairs, 2] with one for each sequence; None: nothing is turned."""
+    if layout not in _PAIRS:
+        raise ValueError("layout is one of " + ", ".join(_PAIRS))
+    first, first_out = next(((x, y) for x, y in ((Q, Qo), (K, Ko), (V, Vo)) if x is not None), (None, None))
+    if first is None or any((x is None) != (y is None) for x, y in ((Q, Qo), (K, Ko), (V, Vo))):
+        raise ValueError("need at least one of Q, K, V, and each with its output")
+    if first.dtype not in _DTYPES or first_out.dtype not in _DTYPES:
+        raise ValueError("inputs and outputs must be float32 or bfloat16")
+    batch, rows, _, d, _ = _heads_of("Q, K or V", first)
+    p = NormRotate(batch, rows, 1, 1, d, _DTYPES[first.dtype], _DTYPES[first_out.dtype], int(norm), 0, _PAIRS[layout], eps, 0, 0)
+    for field, heads, t in (("q", "heads", Q), ("k", "kv_heads", K), ("v", "kv_heads", V)):
+        if t is not None:
+            shape = _heads_of(field.upper(), t)
+            setattr(p, heads, shape[2])
+            setattr(p, field, shape[4])
+    for field, t in (("qo", Qo), ("ko", Ko), ("vo", Vo)):
+        if t is not None:
+            setattr(p, field, _heads_of(field.capitalize(), t)[4])
+    if table is not None:
+        if table.dim() not in (3, 4) or table.shape[-1] != 2:
+            raise ValueError(f"table: need [rows, pairs, 2] or [batch, rows, pairs, 2], got {tuple(table.shape)}")
+        p.pairs = table.shape[-2]
+        p.table_seq = rows * p.pairs if table.dim() == 4 else 0
+    return p
+
+
+def make_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, Out: torch.Tensor, q_span=None, k_span=None, scale: Optional[float] = None,
+                   q_most: Optional[int] = None, k_most: Optional[int] = None) -> Attention:
+    """Descriptor of an attention for tensors laid out like these: [batch, rows, heads, head_dim] (or without batch).  Where a span [batch, 2] is
+    given, Q and Out (or K and V) are [all rows, heads, head_dim] and q_most (k_most) rows the most that a sequence has; by default all.
+    scale: 1 / sqrt(head_dim) by default."""
+    if Q.dtype not in _DTYPES:
+        raise ValueError("Q, K, V and Out must be float32 or bfloat16")
+    nq, rq, heads, d, sq = _heads_of("Q", Q)
+    nk, rk, kv_heads, _, sk = _heads_of("K", K)
+    for name, span, n in (("q_span", q_span, nq), ("k_span", k_span, nk)):
+        if span is not None and n != 1:
+            raise ValueError(f"{name}: tensors with spans are [all rows, heads, head_dim]")
+    batch = q_span.shape[0] if q_span is not None else k_span.shape[0] if k_span is not None else nq
+    return Attention(batch, rq if q_span is None or q_most is None else q_most, rk if k_span is None or k_most is None else k_most, rq, rk, heads, kv_heads, d,
+                     _DTYPES[Q.dtype], d ** -0.5 if scale is None else scale, 0, sq, sk, _heads_of("V", V)[4], _heads_of("Out", Out)[4])
+
+
+def svdcache_rotary_table(p: Rotary, positions, table):
+    """table[row][pair] = (cos, sin) of the pair's angle at the row's positions."""
+    if _fast_call("rotary_table", p, positions, table):
+        return
+    want = torch.int32 if p.whole else torch.float32
+    if positions.dtype != want:
+        raise ValueError(f"positions: dtype {positions.dtype} is not {want}")
+    rows, axes, ld = _row_stride("positions", positions)
+    if (rows, axes) != (p.rows, p.axes) or (rows > 1 and ld != p.ld):
+        raise ValueError(f"positions: {tuple(positions.shape)} with row stride {ld} is not {p.rows} rows of {p.axes} axes with row stride {p.ld}")
+    _dense_f32(p.rows * sum(p.dims[:p.axes]), "[rows, pairs, 2]", table=table)
+    _on_current_device(positions, table)
+    _check(load_library().svdcache_rotary_table(C.byref(p), _ptr(positions), _ptr(table), _stream()), "svdcache_rotary_table")
+
+
+def svdcache_norm_rotate(p: NormRotate, Q, K, V, gain_q, gain_k, table, Qo, Ko, Vo):
+    """Norm and rotation of the heads of Q and K; V is copied.  Outputs may be their inputs."""
+    if _fast_call("norm_rotate", p, Q, K, V, gain_q, gain_k, table, Qo, Ko, Vo):
+        return
+    for name, t, o, heads, s, so in (("Q", Q, Qo, p.heads, p.q, p.qo), ("K", K, Ko, p.kv_heads, p.k, p.ko), ("V", V, Vo, p.kv_heads, p.v, p.vo)):
+        if (t is None) != (o is None):
+            raise ValueError(f"{name} and {name}o go together")
+        if t is not None:
+            _check_heads(name, t, p.batch, p.rows, heads, p.head_dim, s, p.dtype)
+            _check_heads(name + "o", o, p.batch, p.rows, heads, p.head_dim, so, p.dtype_out, out=True)
+    _dense_f32(p.head_dim, "[head_dim]", gain_q=gain_q, gain_k=gain_k)
+    if p.pairs and (Q is not None or K is not None):
+        if table is None:
+            raise ValueError("table: the descriptor's pairs need one")
+        if p.table_seq not in (0, p.rows * p.pairs):
+            raise ValueError("table: tables of sequences lie one behind the other")
+        _dense_f32(p.rows * p.pairs * 2 * (p.batch if p.table_seq else 1), "[rows, pairs, 2]", table=table)
+    _on_current_device(Q, K, V, gain_q, gain_k, table, Qo, Ko, Vo)
+    rc = load_library().svdcache_norm_rotate(C.byref(p), _ptr(Q), _ptr(K), _ptr(V), _ptr(gain_q), _ptr(gain_k), _ptr(table), _ptr(Qo), _ptr(Ko), _ptr(Vo),
+                                             _stream())
+    _check(rc, "svdcache_norm_rotate")
+
+
+def svdcache_attention_workspace_bytes(p: Attention) -> int:
+    return load_library().svdcache_attention_workspace_bytes(C.byref(p))
+
+
+def svdcache_attention(p: Attention, Q, K, V, Out, q_span=None, k_span=None, key_mask=None, workspace=None):
+    """Out = softmax(scale Q K^T) V.  key_mask: a byte or truth value for each key, 0 leaves it out.  workspace: alloc_attention_workspace(p), one
+    for each call in flight on a stream of its own."""
+    if _fast_call("attention", p, Q, K, V, Out, q_span, k_span, key_mask, workspace):
+        return
+    q_shape = (p.batch, p.q_rows) if q_span is None else (1, p.q_total)
+    k_shape = (p.batch, p.k_rows) if k_span is None else (1, p.k_total)
+    _check_heads("Q", Q, *q_shape, p.heads, p.head_dim, p.q, p.dtype)
+    _check_heads("K", K, *k_shape, p.kv_heads, p.head_dim, p.k, p.dtype)
+    _check_heads("V", V, *k_shape, p.kv_heads, p.head_dim, p.v, p.dtype)
+    _check_heads("Out", Out, *q_shape, p.heads, p.head_dim, p.o, p.dtype, out=True)
+    for name, t in (("q_span", q_span), ("k_span", k_span)):
+        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (p.batch, 2) or not t.is_contiguous()):
+            raise ValueError(f"{name}: need a contiguous int32 tensor [{p.batch}, 2], got {t.dtype} {tuple(t.shape)}")
+    if key_mask is not None:
+        need = p.batch * p.k_rows if k_span is None else p.k_total
+        if key_mask.dtype not in (torch.uint8, torch.bool) or not key_mask.is_contiguous() or key_mask.numel() != need:
+            raise ValueError(f"key_mask: need {need} contiguous uint8 or bool, got {key_mask.dtype} {tuple(key_mask.shape)}")
+    _on_current_device(Q, K, V, Out, q_span, k_span, key_mask, workspace)
+    rc = load_library().svdcache_attention(C.byref(p), _ptr(Q), _ptr(K), _ptr(V), _ptr(q_span), _ptr(k_span), _ptr(key_mask), _ptr(Out), _ptr(workspace),
+                                           0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    _check(rc, "svdcache_attention")
+
+
 # ---- conveniences that only allocate (torch owns the memory) ------------------------------------
 
 def fit_basis(F: torch.Tensor, k: int, p: int = 0, q: int = 0, seed: int = 0, max_sweeps: int = 0,
@@ -727,3 +928,34 @@ def matmul8(A, A_scales, W, W_scales, K: int, bias: Optional[torch.Tensor] = Non
         Out, Out_scales = torch.empty(p.M, p.N, device=A.device, dtype=dtype), None
     svdcache_matmul8(p, A, A_scales, W, W_scales, bias, Out, Out_scales, alloc_matmul8_workspace(p, A.device))
     return Out if Out_scales is None else (Out, Out_scales)
+
+
+def rotary_table(positions: torch.Tensor, dims, theta=10000.0):
+    """(cos, sin) of the angles at positions [..., axes] in a new tensor [rows, pairs, 2]."""
+    p = make_rotary(positions, dims, theta)
+    table = torch.empty(p.rows, sum(p.dims[:p.axes]) // 2, 2, device=positions.device)
+    svdcache_rotary_table(p, positions, table)
+    return table
+
+
+def norm_rotate(Q=None, K=None, V=None, gain_q=None, gain_k=None, table=None, layout: str = "neighbours", norm: bool = True, eps: float = 1e-6,
+                dtype: Optional[torch.dtype] = None):
+    """(Qo, Ko, Vo) in new tensors of `dtype` (the inputs' by default), None for what is not given."""
+    out = [None if t is None else torch.empty(t.shape, device=t.device, dtype=dtype or t.dtype) for t in (Q, K, V)]
+    svdcache_norm_rotate(make_norm_rotate(Q, K, V, *out, table, layout, norm, eps), Q, K, V, gain_q, gain_k, table, *out)
+    return tuple(out)
+
+
+def alloc_attention_workspace(p: Attention, device):
+    """Workspace of svdcache_attention for this attention, or None where it needs none."""
+    n = svdcache_attention_workspace_bytes(p)
+    return torch.empty(n, device=device, dtype=torch.uint8) if n else None
+
+
+def attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, scale: Optional[float] = None, q_span=None, k_span=None, key_mask=None,
+              q_most: Optional[int] = None, k_most: Optional[int] = None):
+    """softmax(scale Q K^T) V in a new tensor of Q's shape; rows that no span has are zeros."""
+    Out = (torch.empty if q_span is None else torch.zeros)(Q.shape, device=Q.device, dtype=Q.dtype)
+    p = make_attention(Q, K, V, Out, q_span, k_span, scale, q_most, k_most)
+    svdcache_attention(p, Q, K, V, Out, q_span, k_span, key_mask, alloc_attention_workspace(p, Q.device))
+    return Out

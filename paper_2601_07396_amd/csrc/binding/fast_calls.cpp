@@ -15,8 +15,8 @@
 
 namespace {
 
-// binding.Shape, Norm8, Quant8 and Matmul8
-PyTypeObject *shape_type, *norm8_type, *quant8_type, *matmul8_type;
+// binding.Shape, Norm8, Quant8, Matmul8, Rotary, NormRotate and Attention
+PyTypeObject *shape_type, *norm8_type, *quant8_type, *matmul8_type, *rotary_type, *norm_rotate_type, *attention_type;
 
 // addresses inside the library that the binding loaded
 struct Library {
@@ -31,6 +31,9 @@ struct Library {
   decltype(&svdcache_rms_norm8) rms_norm8;
   decltype(&svdcache_quantize8) quantize8;
   decltype(&svdcache_matmul8) matmul8;
+  decltype(&svdcache_rotary_table) rotary_table;
+  decltype(&svdcache_norm_rotate) norm_rotate;
+  decltype(&svdcache_attention) attention;
 } lib;
 
 // The arguments of one call; `ok` falls when one of them is not ordinary.
@@ -126,6 +129,44 @@ struct Args8 : Arguments<Problem> {
     return eight(o, (n + block_rows - 1) / block_rows * ((blocks(D) + 3) / 4 * 4));
   }
   static int64_t blocks(int64_t D) { return (D + 127) / 128; }
+};
+
+// Tensors of heads, all on the current device.
+template <typename Problem>
+struct ArgsHeads : Arguments<Problem> {
+  using Arguments<Problem>::ok;
+  const c10::DeviceIndex device = c10::hip::current_device();
+
+  ArgsHeads(PyObject* problem, PyTypeObject* type) : Arguments<Problem>(problem, type) {}
+  const at::Tensor* here(PyObject* o) {
+    const at::Tensor* t = this->tensor(o);
+    if (t && t->device().index() != device) ok = false;
+    return ok ? t : nullptr;
+  }
+  // [batch, rows, heads, d], or [rows, heads, d] for one sequence, with these strides where more than one step is made; an output's grow outwards by whole rows
+  // or heads (other orders are for the binding to look at)
+  void* heads(PyObject* o, int64_t batch, int64_t rows, int64_t heads, int64_t d, const svdc_heads& s, int32_t dtype, bool out = false) {
+    const at::Tensor* t = here(o);
+    if (!t) return nullptr;
+    const int64_t n = t->dim(), at = n - 3;
+    ok = (n == 4 || (n == 3 && batch == 1)) && (dtype == SVDC_F32 || dtype == SVDC_BF16) && t->scalar_type() == (dtype == SVDC_F32 ? at::kFloat : at::kBFloat16) &&
+         (n == 3 || t->size(0) == batch) && t->size(at) == rows && t->size(at + 1) == heads && t->size(at + 2) == d && (d == 1 || t->stride(at + 2) == 1) &&
+         (n == 3 || batch <= 1 || t->stride(0) == s.seq) && (rows <= 1 || t->stride(at) == s.row) && (heads <= 1 || t->stride(at + 1) == s.head);
+    if (ok && out) {
+      const int64_t of_heads = heads > 1 ? (heads - 1) * s.head + d : d, of_rows = rows > 1 ? (rows - 1) * s.row + of_heads : of_heads;
+      ok = (heads <= 1 || s.head >= d) && (rows <= 1 || s.row >= of_heads) && (batch <= 1 || s.seq >= of_rows);
+    }
+    return ok ? t->data_ptr() : nullptr;
+  }
+  void* numbers(PyObject* o, int64_t count) {         // contiguous float32
+    return here(o) ? this->dense(o, count) : nullptr;
+  }
+  void* span(PyObject* o, int64_t batch) {
+    const at::Tensor* t = here(o);
+    if (!t) return nullptr;
+    ok = t->scalar_type() == at::kInt && t->dim() == 2 && t->size(0) == batch && t->size(1) == 2 && t->is_contiguous();
+    return ok ? t->data_ptr() : nullptr;
+  }
 };
 
 // Runs `body(args)`, which returns a call to make without the interpreter lock; None where the arguments are not ordinary.
@@ -259,11 +300,64 @@ PyObject* matmul8(PyObject*, PyObject* const* v, Py_ssize_t n) {            // m
   }, matmul8_type);
 }
 
-// bind(addresses of the loaded library's functions by name, the classes of the shape, the norm, the quantisation and the product)
+PyObject* rotary_table(PyObject*, PyObject* const* v, Py_ssize_t n) {       // rotary positions table
+  return call_with<ArgsHeads<svdc_rotary>>(v, n, 3, [&](ArgsHeads<svdc_rotary>& a) {
+    const svdc_rotary& p = a.s;
+    int64_t columns = 0;
+    for (int i = 0; i < SVDC_MAX_AXES && i < p.axes; ++i) columns += p.dims[i];
+    const at::Tensor* t = a.here(v[1]);
+    if (t)
+      a.ok = t->scalar_type() == (p.whole ? at::kInt : at::kFloat) && t->dim() == 2 && t->size(0) == p.rows && t->size(1) == p.axes &&
+             (p.axes == 1 || t->stride(1) == 1) && (p.rows <= 1 || t->stride(0) == p.ld);
+    void *pos = a.ok ? t->data_ptr() : nullptr, *table = a.numbers(v[2], p.rows * columns);
+    return [=, &a](void* st) { return lib.rotary_table(&a.s, pos, (float*)table, st); };
+  }, rotary_type);
+}
+PyObject* norm_rotate(PyObject*, PyObject* const* v, Py_ssize_t n) {        // norm_rotate Q K V gain_q gain_k table Qo Ko Vo
+  return call_with<ArgsHeads<svdc_norm_rotate>>(v, n, 10, [&](ArgsHeads<svdc_norm_rotate>& a) {
+    const svdc_norm_rotate& p = a.s;
+    void *in[3], *out[3];
+    const svdc_heads* strides[6] = {&p.q, &p.k, &p.v, &p.qo, &p.ko, &p.vo};
+    for (int i = 0; i < 3; ++i) {
+      a.ok = a.ok && (v[1 + i] == Py_None) == (v[7 + i] == Py_None);
+      const bool none = v[1 + i] == Py_None;
+      in[i] = none ? nullptr : a.heads(v[1 + i], p.batch, p.rows, i ? p.kv_heads : p.heads, p.head_dim, *strides[i], p.dtype);
+      out[i] = none ? nullptr : a.heads(v[7 + i], p.batch, p.rows, i ? p.kv_heads : p.heads, p.head_dim, *strides[3 + i], p.dtype_out, true);
+    }
+    void *gain_q = v[4] == Py_None ? nullptr : a.numbers(v[4], p.head_dim), *gain_k = v[5] == Py_None ? nullptr : a.numbers(v[5], p.head_dim);
+    a.ok = a.ok && (p.pairs > 0) == (v[6] != Py_None) && (p.table_seq == 0 || p.table_seq == p.rows * p.pairs);
+    void* table = v[6] == Py_None ? nullptr : a.numbers(v[6], 2 * p.rows * p.pairs * (p.table_seq ? p.batch : 1));
+    void *Q = in[0], *K = in[1], *V = in[2], *Qo = out[0], *Ko = out[1], *Vo = out[2];
+    return [=, &a](void* st) { return lib.norm_rotate(&a.s, Q, K, V, (float*)gain_q, (float*)gain_k, (float*)table, Qo, Ko, Vo, st); };
+  }, norm_rotate_type);
+}
+PyObject* attention(PyObject*, PyObject* const* v, Py_ssize_t n) {          // attention Q K V Out q_span k_span key_mask workspace
+  return call_with<ArgsHeads<svdc_attention>>(v, n, 9, [&](ArgsHeads<svdc_attention>& a) {
+    const svdc_attention& p = a.s;
+    const bool qs = v[5] != Py_None, ks = v[6] != Py_None;
+    const int64_t qb = qs ? 1 : p.batch, qr = qs ? p.q_total : p.q_rows, kb = ks ? 1 : p.batch, kr = ks ? p.k_total : p.k_rows;
+    void *Q = a.heads(v[1], qb, qr, p.heads, p.head_dim, p.q, p.dtype), *K = a.heads(v[2], kb, kr, p.kv_heads, p.head_dim, p.k, p.dtype),
+         *V = a.heads(v[3], kb, kr, p.kv_heads, p.head_dim, p.v, p.dtype), *Out = a.heads(v[4], qb, qr, p.heads, p.head_dim, p.o, p.dtype, true);
+    void *q_span = qs ? a.span(v[5], p.batch) : nullptr, *k_span = ks ? a.span(v[6], p.batch) : nullptr;
+    void* mask = nullptr;
+    if (v[7] != Py_None) {
+      const at::Tensor* t = a.here(v[7]);
+      if (t) a.ok = (t->scalar_type() == at::kByte || t->scalar_type() == at::kBool) && t->is_contiguous() && t->numel() == kb * kr;
+      mask = a.ok ? t->data_ptr() : nullptr;
+    }
+    size_t have = 0;
+    void* workspace = v[8] == Py_None || !a.here(v[8]) ? nullptr : a.bytes(v[8], 1, &have);
+    return [=, &a](void* st) {
+      return lib.attention(&a.s, Q, K, V, (int32_t*)q_span, (int32_t*)k_span, (uint8_t*)mask, Out, workspace, have, st);
+    };
+  }, attention_type);
+}
+
+// bind(addresses of the loaded library's functions by name, the classes of the descriptors)
 PyObject* bind(PyObject*, PyObject* args) {
-  PyObject *addresses, *type[4];
-  if (!PyArg_ParseTuple(args, "O!O!O!O!O!", &PyDict_Type, &addresses, &PyType_Type, &type[0], &PyType_Type, &type[1], &PyType_Type, &type[2],
-                        &PyType_Type, &type[3]))
+  PyObject *addresses, *type[7];
+  if (!PyArg_ParseTuple(args, "O!O!O!O!O!O!O!O!", &PyDict_Type, &addresses, &PyType_Type, &type[0], &PyType_Type, &type[1], &PyType_Type, &type[2],
+                        &PyType_Type, &type[3], &PyType_Type, &type[4], &PyType_Type, &type[5], &PyType_Type, &type[6]))
     return nullptr;
   auto get = [&](const char* name) -> void* {
     PyObject* o = PyDict_GetItemString(addresses, name);
@@ -282,16 +376,20 @@ PyObject* bind(PyObject*, PyObject* args) {
   SVDC_BIND(rms_norm8);
   SVDC_BIND(quantize8);
   SVDC_BIND(matmul8);
+  SVDC_BIND(rotary_table);
+  SVDC_BIND(norm_rotate);
+  SVDC_BIND(attention);
 #undef SVDC_BIND
   if (PyErr_Occurred()) return nullptr;
   if (!l.packed_basis_bytes || !l.packed_state_bytes || !l.full_step || !l.full_step_residual_ema || !l.full_step_packed ||
-      !l.forecast || !l.forecast_packed || !l.forecast_combine || !l.rms_norm8 || !l.quantize8 || !l.matmul8) {
+      !l.forecast || !l.forecast_packed || !l.forecast_combine || !l.rms_norm8 || !l.quantize8 || !l.matmul8 || !l.rotary_table || !l.norm_rotate ||
+      !l.attention) {
     PyErr_SetString(PyExc_ValueError, "bind: an address is missing");
     return nullptr;
   }
   lib = l;
-  PyTypeObject** const held[4] = {&shape_type, &norm8_type, &quant8_type, &matmul8_type};
-  for (int i = 0; i < 4; ++i) {
+  PyTypeObject** const held[7] = {&shape_type, &norm8_type, &quant8_type, &matmul8_type, &rotary_type, &norm_rotate_type, &attention_type};
+  for (int i = 0; i < 7; ++i) {
     Py_INCREF(type[i]);
     Py_XDECREF(*held[i]);
     *held[i] = reinterpret_cast<PyTypeObject*>(type[i]);
@@ -308,6 +406,9 @@ PyMethodDef methods[] = {{"full_step", (PyCFunction)(void (*)())full_step, METH_
                          {"rms_norm8", (PyCFunction)(void (*)())rms_norm8, METH_FASTCALL, nullptr},
                          {"quantize8", (PyCFunction)(void (*)())quantize8, METH_FASTCALL, nullptr},
                          {"matmul8", (PyCFunction)(void (*)())matmul8, METH_FASTCALL, nullptr},
+                         {"rotary_table", (PyCFunction)(void (*)())rotary_table, METH_FASTCALL, nullptr},
+                         {"norm_rotate", (PyCFunction)(void (*)())norm_rotate, METH_FASTCALL, nullptr},
+                         {"attention", (PyCFunction)(void (*)())attention, METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast_calls", "Step calls with ordinary arguments.", -1, methods,

@@ -66,6 +66,14 @@ size_t matmul8_workspace_bytes(const svdc_matmul8& p);
 int32_t launch_matmul8(const svdc_matmul8& p, const void* A, const void* As, const void* W, const void* Ws, const float* bias, void* Out, void* Os,
                        void* workspace, hipStream_t st);
 
+// ---- operators around a block's attention: heads_kernels.hip, attention_kernels.hip ---------------
+int32_t launch_rotary_table(const svdc_rotary& p, const void* pos, float* table, hipStream_t st);
+int32_t launch_norm_rotate(const svdc_norm_rotate& p, const void* Q, const void* K, const void* V, const float* gain_q, const float* gain_k,
+                           const float* table, void* Qo, void* Ko, void* Vo, hipStream_t st);
+size_t attention_workspace_bytes(const svdc_attention& p);
+int32_t launch_attention(const svdc_attention& p, const void* Q, const void* K, const void* V, const int32_t* q_span, const int32_t* k_span,
+                         const uint8_t* key_mask, void* Out, void* workspace, hipStream_t st);
+
 // ---- matrix-core kernels: mfma_kernels.hip -----------------------------------
 bool mfma_shape_supported(const svdc_shape& s);
 size_t mfma_packed_bytes(const svdc_shape& s);

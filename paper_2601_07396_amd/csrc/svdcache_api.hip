@@ -51,6 +51,32 @@ int32_t check_matmul8(const svdc_matmul8* p) {
   return SVDC_OK;
 }
 
+// Limits of the operators around the attention.  With rows up to 2^31 and the strides' limits no offset leaves 2^62.
+constexpr int32_t kMaxHeadDim = 256, kMaxHeads = 1 << 16, kMaxTurned = 128;
+constexpr int64_t kMaxRowStride = int64_t(1) << 22, kMaxStride = int64_t(1) << 40;
+bool heads_ok(const svdc_heads& s, bool seq = true) {
+  return s.row >= 0 && s.row <= kMaxRowStride && s.head >= 0 && s.head <= kMaxStride && (!seq || (s.seq >= 0 && s.seq <= kMaxStride));
+}
+bool same_heads(const svdc_heads& a, const svdc_heads& b) { return a.seq == b.seq && a.row == b.row && a.head == b.head; }
+bool batch_rows_ok(int64_t batch, int64_t rows) {
+  return batch >= 0 && batch <= INT32_MAX && rows >= 0 && rows <= INT32_MAX && batch * rows <= INT32_MAX;
+}
+
+int32_t check_attention(const svdc_attention* p, bool q_span, bool k_span) {
+  if (!p) return SVDC_E_NULL;
+  if (!plain_dtype(p->dtype)) return SVDC_E_DTYPE;
+  if (!(p->scale > 0.f && p->scale <= 3.402823466e38f) || p->reserved != 0) return SVDC_E_PARAM;
+  if (p->batch > 65535 || !batch_rows_ok(p->batch, p->q_rows) || !batch_rows_ok(p->batch, p->k_rows) || p->heads < 1 || p->heads > kMaxHeads || p->kv_heads < 1 ||
+      p->heads % p->kv_heads != 0 || p->head_dim < 1 || p->head_dim > kMaxHeadDim)
+    return SVDC_E_SHAPE;
+  // workgroups of a launch, of 128 queries at least, and waves of the one that joins parts
+  if (p->batch * p->heads * ((p->q_rows + 127) / 128) > (1 << 24)) return SVDC_E_SHAPE;
+  if (q_span && (p->q_total < 0 || p->q_total > INT32_MAX)) return SVDC_E_SHAPE;
+  if (k_span && (p->k_total < 0 || p->k_total > INT32_MAX)) return SVDC_E_SHAPE;
+  if (!heads_ok(p->q, !q_span) || !heads_ok(p->o, !q_span) || !heads_ok(p->k, !k_span) || !heads_ok(p->v, !k_span)) return SVDC_E_SHAPE;
+  return SVDC_OK;
+}
+
 constexpr int kMaxDevices = 64;
 void* g_scratch_ptr[kMaxDevices];   // device address of `scratch` on each device, resolved on first use
 std::mutex g_scratch_mutex;
@@ -78,7 +104,7 @@ __global__ void copy_status_kernel(const int32_t* __restrict__ src, int32_t* __r
 
 extern "C" {
 
-int32_t svdcache_version(void) { return 400; }   // 0.4.0: operators of a block in 8 bits
+int32_t svdcache_version(void) { return 500; }   // 0.5.0: operators around a block's attention
 
 const char* svdcache_strerror(int32_t status) {
   switch (status) {
@@ -405,6 +431,71 @@ int32_t svdcache_matmul8(const svdc_matmul8* p, const void* A, const void* A_sca
   if (need && !aligned(workspace, 256)) return SVDC_E_ALIGN;
   if (need > workspace_bytes) return SVDC_E_WORKSPACE;
   return launch_matmul8(*p, A, A_scales, W, W_scales, bias, Out, Out_scales, need ? workspace : nullptr, (hipStream_t)stream);
+}
+
+int32_t svdcache_rotary_table(const svdc_rotary* p, const void* pos, float* table, void* stream) {
+  if (!p) return SVDC_E_NULL;
+  if (p->rows < 0 || p->rows > INT32_MAX || p->axes < 1 || p->axes > SVDC_MAX_AXES || p->ld < p->axes || p->ld > (1 << 24)) return SVDC_E_SHAPE;
+  if (p->whole != 0 && p->whole != 1) return SVDC_E_PARAM;
+  int64_t columns = 0;
+  for (int a = 0; a < p->axes; ++a) {
+    if (p->dims[a] < 2 || p->dims[a] % 2 || p->dims[a] > 2 * kMaxTurned) return SVDC_E_SHAPE;
+    if (!(p->theta[a] > 0.0 && p->theta[a] <= 1.7976931348623157e308)) return SVDC_E_PARAM;
+    columns += p->dims[a];
+  }
+  if (columns > 2 * kMaxTurned) return SVDC_E_SHAPE;
+  if (p->rows == 0) return SVDC_OK;
+  if (!pos || !table) return SVDC_E_NULL;
+  if (!aligned(pos, 4) || !aligned(table, 8)) return SVDC_E_ALIGN;
+  return launch_rotary_table(*p, pos, table, (hipStream_t)stream);
+}
+
+int32_t svdcache_norm_rotate(const svdc_norm_rotate* p, const void* Q, const void* K, const void* V, const float* gain_q, const float* gain_k,
+                             const float* table, void* Qo, void* Ko, void* Vo, void* stream) {
+  if (!p) return SVDC_E_NULL;
+  if (!plain_dtype(p->dtype) || !plain_dtype(p->dtype_out)) return SVDC_E_DTYPE;
+  if (!(p->eps >= 0.f && p->eps <= 3.402823466e38f) || (p->norm != 0 && p->norm != 1) || p->reserved != 0 ||
+      (p->layout != SVDC_PAIRS_NEIGHBOURS && p->layout != SVDC_PAIRS_HALVES))
+    return SVDC_E_PARAM;
+  if (!batch_rows_ok(p->batch, p->rows) || p->heads < 1 || p->heads > kMaxHeads || p->kv_heads < 1 || p->kv_heads > kMaxHeads || p->head_dim < 1 ||
+      p->head_dim > kMaxHeadDim || p->pairs < 0 || 2 * p->pairs > p->head_dim || p->table_seq < 0 || p->table_seq > kMaxStride)
+    return SVDC_E_SHAPE;
+  if ((Q && (!heads_ok(p->q) || !heads_ok(p->qo))) || (K && (!heads_ok(p->k) || !heads_ok(p->ko))) || (V && (!heads_ok(p->v) || !heads_ok(p->vo)))) return SVDC_E_SHAPE;
+  if (p->batch == 0 || p->rows == 0) return SVDC_OK;
+  if ((!Q && !K && !V) || (Q == nullptr) != (Qo == nullptr) || (K == nullptr) != (Ko == nullptr) || (V == nullptr) != (Vo == nullptr) || (p->pairs && (Q || K) && !table))
+    return SVDC_E_NULL;
+  const size_t in = dtype_size(p->dtype), out = dtype_size(p->dtype_out);
+  if (!aligned(Q, in) || !aligned(K, in) || !aligned(V, in) || !aligned(Qo, out) || !aligned(Ko, out) || !aligned(Vo, out) || (p->pairs && !aligned(table, 8)) ||
+      (p->norm && (!aligned(gain_q, 4) || !aligned(gain_k, 4))))
+    return SVDC_E_ALIGN;
+  // in place: a head is written where it was read
+  const bool types = p->dtype == p->dtype_out;
+  if ((Q && Qo == Q && !(types && same_heads(p->q, p->qo))) || (K && Ko == K && !(types && same_heads(p->k, p->ko))) || (V && Vo == V && !(types && same_heads(p->v, p->vo))))
+    return SVDC_E_PARAM;
+  // one buffer for two of the outputs, or one that is another's input
+  if ((Qo && (Qo == Ko || Qo == Vo || Qo == K || Qo == V)) || (Ko && (Ko == Vo || Ko == Q || Ko == V)) || (Vo && (Vo == Q || Vo == K))) return SVDC_E_PARAM;
+  return launch_norm_rotate(*p, Q, K, V, gain_q, gain_k, table, Qo, Ko, Vo, (hipStream_t)stream);
+}
+
+size_t svdcache_attention_workspace_bytes(const svdc_attention* p) {
+  // the strides of a sequence do not change it, and need not be there where spans are given
+  return check_attention(p, false, false) == SVDC_OK || check_attention(p, true, true) == SVDC_OK ? attention_workspace_bytes(*p) : 0;
+}
+
+int32_t svdcache_attention(const svdc_attention* p, const void* Q, const void* K, const void* V, const int32_t* q_span, const int32_t* k_span,
+                           const uint8_t* key_mask, void* Out, void* workspace, size_t workspace_bytes, void* stream) {
+  const int32_t rc = check_attention(p, q_span != nullptr, k_span != nullptr);
+  if (rc != SVDC_OK) return rc;
+  if (p->batch == 0 || p->q_rows == 0) return SVDC_OK;
+  if (!Q || !Out || (p->k_rows && (!K || !V))) return SVDC_E_NULL;
+  const size_t unit = dtype_size(p->dtype);
+  if (!aligned(Q, unit) || !aligned(K, unit) || !aligned(V, unit) || !aligned(Out, unit) || !aligned(q_span, 8) || !aligned(k_span, 8)) return SVDC_E_ALIGN;
+  if (Out == Q || (p->k_rows && (Out == K || Out == V))) return SVDC_E_PARAM;
+  const size_t need = attention_workspace_bytes(*p);
+  if (need && !workspace) return SVDC_E_NULL;
+  if (need && !aligned(workspace, 256)) return SVDC_E_ALIGN;
+  if (need > workspace_bytes) return SVDC_E_WORKSPACE;
+  return launch_attention(*p, Q, K, V, q_span, k_span, key_mask, Out, need ? workspace : nullptr, (hipStream_t)stream);
 }
 
 }  // extern "C"
