@@ -7,6 +7,7 @@
 //     O^T [columns x queries] = V^T P^T   whose right operand wants from lane l numbers of query l % 32, and which numbers of the summed axis is free as
 //                                         long as the left operand has the same: the keys that the lane has.  P goes from one product into the other in registers.
 #include <algorithm>
+#include <type_traits>
 
 #include "attention_plan.h"
 #include "eight_bit.h"
@@ -18,6 +19,8 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+#define INLINE __attribute__((always_inline))
 
 struct AttentionArgs {
   const void *Q, *K, *V;
@@ -31,7 +34,13 @@ struct AttentionArgs {
   float scale;                       // times log2 e
 };
 
+// what all lanes hold, as a scalar
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+template <typename T>
+__device__ __forceinline__ T* uniform(T* p) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<T*>((uint64_t)(uint32_t)uniform((int)(u >> 32)) << 32 | (uint32_t)uniform((int)u));
+}
 
 // Rows of sequence b: the span's, as far as it lies within `total` rows, at most `most`
 struct Rows {
@@ -74,10 +83,11 @@ struct Tile {
   __device__ static __forceinline__ int value_swizzle(int row) { return F32 ? (row >> 2 & 1) << 3 : PITCH == 8 ? (row >> 1 & 1) << 2 : (row & 3) << 2; }
 };
 
+constexpr int WAVES = kTileQueries / 32;                       // of a workgroup
+
 template <int BYTES>
-struct Stage {
-  __align__(1024) uint8_t k[BYTES];
-  __align__(1024) uint8_t v[BYTES];
+struct Lds {
+  __align__(1024) uint8_t b[BYTES];
 };
 
 // Four columns of 16-bit numbers from four rows, transposed: lane i of 16 hands over the address of columns 4 (i % 4) .. + 3 of row i / 4 and gets
@@ -124,43 +134,48 @@ __device__ __forceinline__ void store_columns<bf16_t>(bf16_t* row, int column, i
 }
 
 // DIRECT: head_dim, strides and pointers are multiples of 16 bytes, and tiles are loaded straight into LDS.
-template <typename T, int W, int WAVES, bool DIRECT>
+template <typename T, int W, bool DIRECT, bool MASKED>
 __device__ __forceinline__ void attend(const AttentionArgs& a) {
   using G = Tile<T, W>;
   constexpr int KEYS = G::KEYS, BLOCKS = G::BLOCKS, PITCH = G::PITCH, E = 16 / (int)sizeof(T);
-  constexpr int STAGES = !DIRECT || WAVES == 4 || 6 * G::BYTES > (96 << 10) ? 2 : 3;
   constexpr int LOADS = KEYS * PITCH / (64 * WAVES);          // of each operand, a wave and tile
+  constexpr uint64_t ALL = KEYS == 64 ? ~0ull : 0xffffffffull;
   static_assert(LOADS * 64 * WAVES == KEYS * PITCH, "");
-  __shared__ Stage<G::BYTES> stage0;
-  __shared__ Stage<G::BYTES> stage1;
-  __shared__ Stage<G::BYTES> stage2;                          // not there with two stages
-  Stage<G::BYTES>* const stages[3] = {&stage0, &stage1, STAGES == 3 ? &stage2 : &stage0};
+  __shared__ Lds<G::BYTES> columns0, columns1, keys0, keys1;  // two stages of values and of keys
 
+  constexpr int HEADS_AT_ONCE = 8;
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
-  // Workgroups go round the eight dies in turn; each die gets a run of them, so that the ones at work on it at a time share keys in its cache.
-  int id;
+  // Workgroups go round the eight dies in turn; each die gets a run of them, HEADS_AT_ONCE heads side by side and then the next rows of these heads: the ones at work on
+  // a die at a time share keys in its cache, and where heads lie side by side in a row they do not all ask the same of its channels.
+  int q_tile, part, head, b;
   {
-    const int all = gridDim.x, each = all / 8, more = all % 8, die = blockIdx.x % 8;
-    id = uniform(die * each + min(die, more) + blockIdx.x / 8);
+    const int all = gridDim.x, each = all / 8, more = all % 8, die = blockIdx.x % 8, of_head = a.q_tiles * a.parts;
+    int id = die * each + min(die, more) + blockIdx.x / 8;
+    b = uniform(id / (of_head * a.heads));
+    id -= b * of_head * a.heads;
+    const int first = id / (of_head * HEADS_AT_ONCE) * HEADS_AT_ONCE, side = min(HEADS_AT_ONCE, a.heads - first);
+    id -= first * of_head;
+    head = uniform(first + id % side);
+    q_tile = uniform(id / side % a.q_tiles);
+    part = uniform(id / side / a.q_tiles);
   }
-  const int q_tile = id % a.q_tiles, part = id / a.q_tiles % a.parts, head = id / (a.q_tiles * a.parts) % a.heads, b = id / (a.q_tiles * a.parts * a.heads);
   const Rows queries(a.q_span, b, a.q_total, a.q_rows), keys(a.k_span, b, a.k_total, a.k_rows);
-  const int q0 = q_tile * 32 * WAVES;
+  const int q0 = q_tile * kTileQueries;
   if (q0 >= queries.count) return;
   const int mine = q0 + 32 * wave + r;                        // this lane's query
   const bool there = mine < queries.count;
   const int k_count = uniform(keys.count);
   const int from = uniform(part * a.tiles_of_part), to = uniform(min(from + a.tiles_of_part, (k_count + KEYS - 1) / KEYS));
 
-  const T* K = static_cast<const T*>(a.K) + ((a.k_span ? 0 : b * a.k.seq) + keys.first * a.k.row + (head / a.share) * a.k.head);
-  const T* V = static_cast<const T*>(a.V) + ((a.k_span ? 0 : b * a.v.seq) + keys.first * a.v.row + (head / a.share) * a.v.head);
-  const uint8_t* mask = a.mask ? a.mask + (a.k_span ? keys.first : (int64_t)b * a.k_rows) : nullptr;
+  const int kv_head = uniform(head / a.share);
+  const T* K = uniform(static_cast<const T*>(a.K) + ((a.k_span ? 0 : b * a.k.seq) + keys.first * a.k.row + kv_head * a.k.head));
+  const T* V = uniform(static_cast<const T*>(a.V) + ((a.k_span ? 0 : b * a.v.seq) + keys.first * a.v.row + kv_head * a.v.head));
 
   // ---- tiles of keys and values ----
   const int k_row = uniform((int)(a.k.row * sizeof(T))), v_row = uniform((int)(a.v.row * sizeof(T)));
   const int row_bytes = a.head_dim * (int)sizeof(T);
   uint32_t k_from[LOADS], v_from[LOADS];
-  u32x4 kept_k[DIRECT ? 1 : LOADS], kept_v[DIRECT ? 1 : LOADS];
+  u32x4 kept[DIRECT ? 1 : LOADS];
 #pragma unroll
   for (int n = 0; n < LOADS; ++n) {
     const int slot = (n * WAVES + wave) * 64 + lane, row = slot / PITCH, c = slot % PITCH;
@@ -168,18 +183,39 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
     k_from[n] = kc < row_bytes ? (uint32_t)(row * k_row + kc) : 0x80000000u;      // out of bounds
     v_from[n] = vc < row_bytes ? (uint32_t)(row * v_row + vc) : 0x80000000u;
   }
-  // Direct loads are bounds-checked: rows behind the last key are none of memory.
-  const auto fetch = [&](int tile, Stage<G::BYTES>& stage) {
-    const int rows = uniform(tile < to ? min(KEYS, k_count - tile * KEYS) : 0);
-    const auto Kb = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(K + (int64_t)tile * KEYS * a.k.row), 0, rows ? (rows - 1) * k_row + row_bytes : 0, 0x00027000);
-    const auto Vb = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(V + (int64_t)tile * KEYS * a.v.row), 0, rows ? (rows - 1) * v_row + row_bytes : 0, 0x00027000);
+  // Which keys of a tile take part, a bit each.  The mask's bytes are loaded a step before they are looked at.
+  const auto mask = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(MASKED ? uniform(a.mask + (a.k_span ? keys.first : (int64_t)b * a.k_rows)) : nullptr), 0,
+                                                      MASKED ? k_count : 0, 0x00027000);
+  const auto mask_byte = [&](int tile) INLINE -> int {               // none behind the last key
+    return MASKED ? __builtin_amdgcn_raw_buffer_load_b8(mask, lane < KEYS ? tile * KEYS + lane : -1, 0, 0) : 0;
+  };
+  const auto present = [&](int tile, int byte) INLINE -> uint64_t {
+    if (MASKED) return __builtin_amdgcn_ballot_w64(byte != 0);
+    const int count = k_count - tile * KEYS;
+    return count >= KEYS ? ALL : (1ull << max(0, count)) - 1;
+  };
+  // Direct loads are bounds-checked, and give zeros for rows behind the last key and, by an address out of bounds, for keys left out: a probability of zero
+  // would not make nothing of a NaN.
+  const auto tile_of = [&](const T* rows, int64_t stride, int bytes, int tile) INLINE {
+    const int count = tile < to ? min(KEYS, k_count - tile * KEYS) : 0;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(rows + (int64_t)tile * KEYS * stride), 0, uniform(count ? (count - 1) * bytes + row_bytes : 0), 0x00027000);
+  };
+  const auto fetch = [&](__amdgpu_buffer_rsrc_t tile, uint32_t at, int n, uint64_t keep, uint8_t* stage) INLINE {
+    if (MASKED && !(keep >> ((n * WAVES + wave) * 64 + lane) / PITCH & 1)) at = 0x80000000u;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(tile, stage + (n * WAVES + wave) * 1024, 16, at, 0, 0, 0);
+  };
+  const auto fetch_keys = [&](int tile, uint64_t keep, uint8_t* stage) INLINE {
+    const auto from_here = tile_of(K, a.k.row, k_row, tile);
 #pragma unroll
-    for (int n = 0; n < LOADS; ++n) __builtin_amdgcn_raw_ptr_buffer_load_lds(Kb, stage.k + (n * WAVES + wave) * 1024, 16, k_from[n], 0, 0, 0);
+    for (int n = 0; n < LOADS; ++n) fetch(from_here, k_from[n], n, keep, stage);
+  };
+  const auto fetch_values = [&](int tile, uint64_t keep, uint8_t* stage) INLINE {
+    const auto from_here = tile_of(V, a.v.row, v_row, tile);
 #pragma unroll
-    for (int n = 0; n < LOADS; ++n) __builtin_amdgcn_raw_ptr_buffer_load_lds(Vb, stage.v + (n * WAVES + wave) * 1024, 16, v_from[n], 0, 0, 0);
+    for (int n = 0; n < LOADS; ++n) fetch(from_here, v_from[n], n, keep, stage);
   };
   // The same through registers, at any alignment and width.
-  const auto chunk_of = [&](const T* rows, int64_t row_stride, int row, int c, int count) {
+  const auto chunk_of = [&](const T* rows, int64_t row_stride, int row, int c, int count) INLINE {
     u32x4 w = {};
     const int column = c * E;
     if (row < count && column < a.head_dim) {
@@ -199,46 +235,41 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
     }
     return w;
   };
-  const auto take = [&](int tile) {
-    const int count = tile < to ? k_count - tile * KEYS : 0;
+  const auto take = [&](const T* rows, int64_t stride, int tile, uint64_t keep, auto&& swizzle) INLINE {
 #pragma unroll
-    for (int n = 0; n < LOADS && !DIRECT; ++n) {
+    for (int n = 0; n < LOADS; ++n) {
       const int slot = (n * WAVES + wave) * 64 + lane, row = slot / PITCH, c = slot % PITCH;
-      kept_k[n] = chunk_of(K + (int64_t)tile * KEYS * a.k.row, a.k.row, row, c ^ G::key_swizzle(row), count);
-      kept_v[n] = chunk_of(V + (int64_t)tile * KEYS * a.v.row, a.v.row, row, c ^ G::value_swizzle(row), count);
+      kept[n] = chunk_of(rows + (int64_t)tile * KEYS * stride, stride, row, c ^ swizzle(row), tile < to && (keep >> row & 1) ? row + 1 : 0);
     }
   };
-  const auto put = [&](Stage<G::BYTES>& stage) {
+  const auto take_keys = [&](int tile, uint64_t keep) INLINE { take(K, a.k.row, tile, keep, G::key_swizzle); };
+  const auto take_values = [&](int tile, uint64_t keep) INLINE { take(V, a.v.row, tile, keep, G::value_swizzle); };
+  const auto put = [&](uint8_t* stage) INLINE {
 #pragma unroll
-    for (int n = 0; n < LOADS && !DIRECT; ++n) {
-      const int slot = (n * WAVES + wave) * 64 + lane;
-      *reinterpret_cast<u32x4*>(stage.k + slot * 16) = kept_k[n];
-      *reinterpret_cast<u32x4*>(stage.v + slot * 16) = kept_v[n];
+    for (int n = 0; n < LOADS; ++n) *reinterpret_cast<u32x4*>(stage + ((n * WAVES + wave) * 64 + lane) * 16) = kept[n];
+  };
+  // The last tile lies in stage 0.
+  const int steps = max(0, to - from - 1), first = uniform(steps % 2);
+  const auto keys_at = [&](int i) INLINE -> uint8_t* { return i % 2 ? keys1.b : keys0.b; };
+  const auto values_at = [&](int i) INLINE -> uint8_t* { return i % 2 ? columns1.b : columns0.b; };
+  uint64_t keep[4];                                           // of this step's tile and the next ones
+  int byte = 0;
+  if (from < to) {
+    int bytes[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) bytes[i] = mask_byte(from + i);
+    byte = mask_byte(from + 3);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) keep[i] = present(from + i, bytes[i]);
+    if (DIRECT) {
+      fetch_keys(from, keep[0], keys_at(first));
+      fetch_keys(from + 1, keep[1], keys_at(first + 1));
+      fetch_values(from, keep[0], values_at(first));
+    } else {
+      take_keys(from, keep[0]), put(keys_at(first));
+      take_keys(from + 1, keep[1]), put(keys_at(first + 1));
+      take_values(from, keep[0]), put(values_at(first));
     }
-  };
-  // Which keys of a tile take part, a bit each
-  const auto present = [&](int tile) -> uint64_t {
-    const int count = k_count - tile * KEYS;
-    const uint64_t all = KEYS == 64 ? ~0ull : 0xffffffffull;
-    if (!mask) return count >= KEYS ? all : (1ull << count) - 1;
-    const bool in = lane < min(KEYS, count) && mask[(int64_t)tile * KEYS + lane];
-    return __builtin_amdgcn_ballot_w64(in);
-  };
-
-  if (DIRECT && row_bytes != PITCH * 16) {
-    // columns behind the last one are multiplied by zeros: they hold numbers
-    uint32_t* const z[3] = {reinterpret_cast<uint32_t*>(stages[0]), reinterpret_cast<uint32_t*>(stages[1]), reinterpret_cast<uint32_t*>(stages[2])};
-#pragma unroll
-    for (int s = 0; s < STAGES; ++s)
-      for (int i = threadIdx.x; i < (int)sizeof(Stage<G::BYTES>) / 16; i += 64 * WAVES) reinterpret_cast<u32x4*>(z[s])[i] = u32x4{};
-    __syncthreads();
-  }
-  if (DIRECT) {
-    fetch(from, *stages[0]);
-    if (STAGES == 3) fetch(from + 1, *stages[1]);
-  } else {
-    take(from);
-    put(*stages[0]);
   }
 
   // ---- queries, as right operands ----
@@ -251,7 +282,16 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
   }
 
   f32x16 o[W / 32] = {};
-  float top = -INFINITY, top_scaled = 0.f, sum = 0.f;
+  f32x16 s0[BLOCKS], s1[BLOCKS];                              // products of this tile's keys and of the next one's, in turns
+  u32x4 p[2 * BLOCKS];                                        // probabilities of this tile: 2^(product scale log2 e - shift), in bfloat16
+  f32x16 exact_p[BLOCKS];                                     // or in float32
+  // Their sums.  bfloat16: made by a 16 x 16 product, for which lanes 16 g .. 16 g + 15 are columns 0 .. 15 with eight numbers of the summed axis each.  Ones in row 0 for even g,
+  // which hold queries 0 .. 15, and in row 1 for odd g, which hold queries 16 .. 31: lane n's sums[0] is query n's, sums[1] query 16 + n's.
+  float shift = -INFINITY, sum = 0.f;
+  f32x4 sums = {};
+  int lost = 0;
+  const uint32_t one_here = lane % 16 == lane / 16 % 2 ? 0x3f803f80u : 0u;
+  const u32x4 ones = {one_here, one_here, one_here, one_here};
   // addresses in a tile: of this lane's 16 bytes of keys, and of what it reads of values
   const int key_at = r * PITCH * 16, key_sw = G::key_swizzle(r);
   int value_at[W / 32];
@@ -265,113 +305,223 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
     }
   }
 
-  const auto step = [&](int tile, Stage<G::BYTES>& now, Stage<G::BYTES>& next) {
-    if (DIRECT)
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * 2 * LOADS) : "memory");
-    else
-      __syncthreads();
-    const uint64_t keep = present(tile);
-    if (DIRECT)
-      fetch(tile + STAGES - 1, next);
-    else
-      take(tile + 1);
-    const bool whole = keep == (KEYS == 64 ? ~0ull : 0xffffffffull);
-    if (keep) {
-      if (!whole) {
-        // values of keys left out count as zeros: a probability of zero does not make nothing of a NaN
-        for (int i = threadIdx.x; i < KEYS * PITCH; i += 64 * WAVES)
-          if (!(keep >> i / PITCH & 1)) reinterpret_cast<u32x4*>(now.v)[i] = u32x4{};
-        __syncthreads();
+  // The products of a step are dealt out over the softmax's other work, so that both units are busy: `between(n, all)` does the n-th of `all` shares of it behind the n-th
+  // product.  Operands are read from LDS AHEAD products ahead, the first ones before the step's barrier or the other products' end.
+  constexpr int AHEAD = 3;
+  constexpr int KEY_PRODUCTS = STEPS * BLOCKS, VALUE_PRODUCTS = G::F32 ? 16 * BLOCKS : 2 * BLOCKS * (W / 32);
+  u32x4 k[AHEAD + 1];
+  bf16x8 v[AHEAD + 1];
+  const auto read_key = [&](const uint8_t* stage, int n) INLINE {
+    k[n % (AHEAD + 1)] = *reinterpret_cast<const u32x4*>(stage + key_at + 32 * (n % BLOCKS) * PITCH * 16 + ((2 * (n / BLOCKS) + h) ^ key_sw) * 16);
+  };
+  const auto read_value = [&](const uint8_t* stage, int n) INLINE {
+    constexpr int D = W / 32;
+    const uint8_t* at = stage + value_at[n % D] + 16 * (n / D) * PITCH * 16;
+    if (!G::F32) v[n % (AHEAD + 1)] = __builtin_shufflevector(read_transposed(at), read_transposed(at + 8 * PITCH * 16), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  const auto first_keys = [&](const uint8_t* stage) INLINE {
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) read_key(stage, n);
+  };
+  const auto first_values = [&](const uint8_t* stage) INLINE {
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) read_value(stage, n);
+  };
+  const auto multiply_keys = [&](f32x16 (&s)[BLOCKS], const uint8_t* stage, auto&& between) INLINE {
+    constexpr int N = KEY_PRODUCTS;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if (n + AHEAD < N) read_key(stage, n + AHEAD);
+      const int x = n / BLOCKS, t = n % BLOCKS;
+      const u32x4 w = k[n % (AHEAD + 1)];
+      f32x16 c = {};
+      if (x) c = s[t];
+      if (G::F32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w[e]), __uint_as_float(q[x][e]), c, 0, 0, 0);
+      } else {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, q[x]), c, 0, 0, 0);
       }
-      f32x16 s[BLOCKS] = {};
+      s[t] = c;
+      between(n, N);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  const auto multiply_values = [&](const uint8_t* stage) INLINE {
+    constexpr int D = W / 32, N = VALUE_PRODUCTS;
 #pragma unroll
-      for (int x = 0; x < STEPS; ++x)
+    for (int n = 0; n < N; ++n) {
+      if constexpr (G::F32) {
+        const int t = n / 16, i = n % 16;
+        sum += exact_p[t][i];
 #pragma unroll
-        for (int t = 0; t < BLOCKS; ++t) {
-          const u32x4 k = *reinterpret_cast<const u32x4*>(now.k + key_at + 32 * t * PITCH * 16 + ((2 * x + h) ^ key_sw) * 16);
-          if (G::F32) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[c]), __uint_as_float(q[x][c]), s[t], 0, 0, 0);
-          } else {
-            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[x]), s[t], 0, 0, 0);
-          }
+        for (int d = 0; d < D; ++d) {
+          const float v = *reinterpret_cast<const float*>(stage + value_at[d] + (32 * t + 8 * (i / 4) + i % 4) * PITCH * 16);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, exact_p[t][i], o[d], 0, 0, 0);
         }
-      if (!whole) {
-#pragma unroll
-        for (int t = 0; t < BLOCKS; ++t) {
-          const uint32_t bits = (uint32_t)(keep >> 32 * t) >> 4 * h;
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (!(bits >> (8 * (i / 4) + i % 4) & 1)) s[t][i] = -INFINITY;
-        }
-      }
-      float high = s[0][0];
-#pragma unroll
-      for (int t = 0; t < BLOCKS; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) high = fmaxf(high, s[t][i]);
-      high = max_of_halves(high);
-      // The maximum that is subtracted may be any number near the true one: it follows only where probabilities would pass 2^8
-      if (__builtin_amdgcn_ballot_w64(high * a.scale > top_scaled + 8.f || (top == -INFINITY && high > -INFINITY))) {
-        const float next_top = fmaxf(top, high);
-        const float less = next_top == top ? 1.f : __builtin_amdgcn_exp2f((top - next_top) * a.scale);
-        sum *= less;
-#pragma unroll
-        for (int d = 0; d < W / 32; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] *= less;
-        top = next_top;
-        top_scaled = top == -INFINITY ? 0.f : top * a.scale;
-      }
-#pragma unroll
-      for (int t = 0; t < BLOCKS; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], a.scale, -top_scaled));
-          sum += s[t][i];
-        }
-#pragma unroll
-      for (int t = 0; t < BLOCKS; ++t) {
-        if (G::F32) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-#pragma unroll
-            for (int d = 0; d < W / 32; ++d) {
-              const float v = *reinterpret_cast<const float*>(now.v + value_at[d] + (32 * t + 8 * (i / 4) + i % 4) * PITCH * 16);
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[t][i], o[d], 0, 0, 0);
-            }
-        } else {
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            u32x4 p;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = pack_bf16(s[t][8 * x + 2 * i], s[t][8 * x + 2 * i + 1]);
-#pragma unroll
-            for (int d = 0; d < W / 32; ++d) {
-              const uint8_t* at = now.v + value_at[d] + (32 * t + 16 * x) * PITCH * 16;
-              const bf16x4 lo = read_transposed(at), hi = read_transposed(at + 8 * PITCH * 16);
-              const bf16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, p), o[d], 0, 0, 0);
-            }
-          }
-        }
+      } else {
+        if (n + AHEAD < N) read_value(stage, n + AHEAD);
+        if (n % D == 0) sums = mfma16(ones, p[n / D], sums);
+        o[n % D] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[n % (AHEAD + 1)], __builtin_bit_cast(bf16x8, p[n / D]), o[n % D], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (!DIRECT) put(next);
   };
-  for (int tile = from; tile < to; tile += STAGES) {
-    step(tile, *stages[0], *stages[STAGES - 1]);
-    if (tile + 1 < to) step(tile + 1, *stages[1], *stages[0]);
-    if (STAGES == 3 && tile + 2 < to) step(tile + 2, *stages[2], *stages[1]);
-  }
-  if (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing lands in LDS behind the workgroup's end
+  // Probabilities of this tile.  A pair of them comes into being over three shares of the work, so that nothing waits for what was begun just before: exponents, powers, and
+  // what the product takes.  `over` gathers the exponents' highest bit, which numbers from 2 on have (and what is no number).
+  constexpr int PAIRS = 8 * BLOCKS;
+  uint32_t over;
+  float x[2][2];                                              // exponents and powers on their way
+  const auto exponents = [&](const f32x16 (&s)[BLOCKS], float by, int m) INLINE {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      x[m % 2][e] = __builtin_fmaf(s[m / 8][2 * (m % 8) + e], a.scale, -by);
+      asm volatile("" : "+v"(x[m % 2][e]));                    // here, and not where the compiler would move it
+    }
+  };
+  float y[2][2];
+  const auto powers = [&](int m) INLINE {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      y[m % 2][e] = __builtin_amdgcn_exp2f(x[m % 2][e]);
+      asm volatile("" : "+v"(y[m % 2][e]));
+    }
+  };
+  const auto operands = [&](int m) INLINE {
+    if (m == 0) over = 0;
+    if (G::F32) {
+      exact_p[m / 8][2 * (m % 8)] = y[m % 2][0], exact_p[m / 8][2 * (m % 8) + 1] = y[m % 2][1];
+      over |= __float_as_uint(y[m % 2][0]) | __float_as_uint(y[m % 2][1]);
+    } else {
+      uint32_t w = pack_bf16(y[m % 2][0], y[m % 2][1]);
+      asm volatile("" : "+v"(w));
+      p[m / 4][m % 4] = w;
+      over |= w;
+    }
+  };
+  // the n-th of `all` shares, and what is left behind the last one
+  const auto probabilities = [&](const f32x16 (&s)[BLOCKS], float by, int n, int all) INLINE {
+#pragma unroll
+    for (int m = n * PAIRS / all; m < (n + 1) * PAIRS / all; ++m) {
+      if (m == 0) exponents(s, by, 0);
+      if (m >= 1) operands(m - 1);
+      powers(m);
+      if (m + 1 < PAIRS) exponents(s, by, m + 1);
+      if (m + 1 == PAIRS) operands(m);
+    }
+  };
+  const auto leave_out = [&](f32x16 (&s)[BLOCKS], uint64_t keep) INLINE {
+#pragma unroll
+    for (int t = 0; t < BLOCKS; ++t) {
+      const uint32_t bits = (uint32_t)(keep >> 32 * t) >> 4 * h;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!(bits >> (8 * (i / 4) + i % 4) & 1)) s[t][i] = -INFINITY;
+    }
+  };
+  // What is subtracted from the exponents may be any number not far from the maximum: it stays until a probability passes 2, then follows to SLACK above the maximum, and the
+  // tile's probabilities are made again.  -infinity until there is a key: then everything passes.
+  constexpr float SLACK = 6.f;
+  const auto follow = [&](const f32x16 (&s)[BLOCKS]) INLINE {
+    if (__builtin_amdgcn_ballot_w64((over & (G::F32 ? 0x40000000u : 0x40004000u)) != 0) == 0) return;
+    float high = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) high = fmaxf(high, s[t][i]);
+    high = max_of_halves(high) * a.scale;
+    const bool up = !(high - shift < 0.5f);                    // 2 and what rounds to it is well above: behind this, only what is no number still passes
+    const float before = shift;
+    if (up) shift = high + SLACK;
+    const float less = !up ? 1.f : before == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(before - shift);
+    sum *= less;
+    sums[0] *= less;
+    sums[1] *= __shfl(less, lane % 16 + 16);
+#pragma unroll
+    for (int d = 0; d < W / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] *= less;
+    const float by = shift == -INFINITY ? 0.f : shift;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) probabilities(s, by, n, 8);
+    if (!G::F32 && (over & 0x40004000u)) {                     // no number: not into a column that another query's sum comes from, but into the result
+      lost = 1;
+#pragma unroll
+      for (int i = 0; i < 2 * BLOCKS; ++i) p[i] = u32x4{};
+    }
+  };
+  const auto nothing = [](int, int) INLINE {};
+  // Begins a step: all waves have what they asked for in the last one, and are done with what they read in it.
+  const auto begin = [&]() INLINE {
+    if (DIRECT)
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else
+      __syncthreads();
+  };
 
-  sum = sum_of_halves(sum);
+  if (from < to) {
+    begin();
+    first_keys(keys_at(first));
+    multiply_keys(s0, keys_at(first), nothing);
+    if (keep[0] != ALL) leave_out(s0, keep[0]);
+    // Tile by tile: its probabilities beside the products of the next one's keys, then its products with the values.  The stages of its keys and of the values of the tile before
+    // are free and loaded anew, a load here and there: at once they would hold up the wave.
+    const auto step = [&](int tile, uint8_t* keys_now, const uint8_t* keys_next, const uint8_t* values_now, uint8_t* values_next, f32x16 (&s)[BLOCKS],
+                          f32x16 (&s_next)[BLOCKS]) INLINE {
+      begin();
+      first_keys(keys_next);
+      keep[3] = present(tile + 3, byte);
+      byte = mask_byte(tile + 4);
+      const auto keys_tile = tile_of(K, a.k.row, k_row, tile + 2), values_tile = tile_of(V, a.v.row, v_row, tile + 1);
+      if (!DIRECT) take_keys(tile + 2, keep[2]);
+      multiply_keys(s_next, keys_next, [&](int n, int all) INLINE {
+        probabilities(s, shift, n, all);
+#pragma unroll
+        for (int j = n * 2 * LOADS / all; DIRECT && j < (n + 1) * 2 * LOADS / all; ++j) {
+          if (j < LOADS)
+            fetch(values_tile, v_from[j % LOADS], j % LOADS, keep[1], values_next);
+          else
+            fetch(keys_tile, k_from[j % LOADS], j % LOADS, keep[2], keys_now);
+        }
+      });
+      first_values(values_now);
+      follow(s);
+      if (!DIRECT) put(keys_now), take_values(tile + 1, keep[1]);
+      if (keep[1] != ALL) leave_out(s_next, keep[1]);
+      multiply_values(values_now);
+      if (!DIRECT) put(values_next);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) keep[i] = keep[i + 1];
+    };
+    int tile = from;
+    if (first) {
+      step(tile++, keys1.b, keys0.b, columns1.b, columns0.b, s0, s1);
+#pragma unroll
+      for (int t = 0; t < BLOCKS; ++t) s0[t] = s1[t];
+    }
+    while (tile + 1 < to) {
+      step(tile++, keys0.b, keys1.b, columns0.b, columns1.b, s0, s1);
+      step(tile++, keys1.b, keys0.b, columns1.b, columns0.b, s1, s0);
+    }
+    begin();
+#pragma unroll
+    for (int n = 0; n < 8; ++n) probabilities(s0, shift, n, 8);
+    follow(s0);
+    first_values(columns0.b);
+    multiply_values(columns0.b);
+  }
+
+  if (G::F32) {
+    sum = sum_of_halves(sum);
+  } else {
+    const float x = __shfl(sums[0], lane % 16), y = __shfl(sums[1], lane % 16);
+    sum = lost | __shfl_xor(lost, 32) ? NAN : lane & 16 ? y : x;
+  }
   if (!there) return;
   if (a.parts > 1) {
     const int64_t at = (((int64_t)b * a.heads + head) * a.parts + part) * a.q_rows + mine;
     if (h == 0) {
-      a.stats[2 * at] = sum == 0.f ? -INFINITY : top_scaled;   // a sum that is no number counts
+      a.stats[2 * at] = sum == 0.f ? -INFINITY : fmaxf(shift, -3.4e38f);   // a sum that is no number counts
       a.stats[2 * at + 1] = sum;
     }
 #pragma unroll
@@ -388,10 +538,10 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
   }
 }
 
-template <typename T, int W, int WAVES, bool DIRECT>
-__global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attention_kernel(AttentionArgs a) {
+template <typename T, int W, bool DIRECT, bool MASKED>
+__global__ __launch_bounds__(64 * WAVES, W <= 128 && DIRECT ? 2 : 1) void attention_kernel(AttentionArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__          // buffer descriptors mean nothing to the host's pass
-  attend<T, W, WAVES, DIRECT>(a);
+  attend<T, W, DIRECT, MASKED>(a);
 #endif
 }
 
@@ -431,24 +581,25 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
     if (64 * e + lane < a.head_dim) st_elem(Out, 64 * e + lane, o[e] * share);
 }
 
+template <typename T, int W, bool DIRECT>
+void attention_masked(const AttentionArgs& a, unsigned grid, hipStream_t st) {
+  a.mask ? attention_kernel<T, W, DIRECT, true><<<grid, 64 * WAVES, 0, st>>>(a) : attention_kernel<T, W, DIRECT, false><<<grid, 64 * WAVES, 0, st>>>(a);
+}
+
 template <typename T, int W>
-void attention_of(const AttentionArgs& a, const AttentionPlan& plan, bool direct, hipStream_t st) {
-  const unsigned grid = (unsigned)((int64_t)a.batch * a.heads * a.q_tiles * plan.parts);
-  if (plan.waves == 8) {
-    if constexpr (W <= 128) direct ? attention_kernel<T, W, 8, true><<<grid, 512, 0, st>>>(a) : attention_kernel<T, W, 8, false><<<grid, 512, 0, st>>>(a);
-  } else {
-    direct ? attention_kernel<T, W, 4, true><<<grid, 256, 0, st>>>(a) : attention_kernel<T, W, 4, false><<<grid, 256, 0, st>>>(a);
-  }
-  if (plan.parts > 1) attention_join_kernel<T, W><<<(unsigned)(((int64_t)a.batch * a.heads * a.q_rows + 3) / 4), 256, 0, st>>>(a);
+void attention_of(const AttentionArgs& a, bool direct, hipStream_t st) {
+  const unsigned grid = (unsigned)((int64_t)a.batch * a.heads * a.q_tiles * a.parts);
+  direct ? attention_masked<T, W, true>(a, grid, st) : attention_masked<T, W, false>(a, grid, st);
+  if (a.parts > 1) attention_join_kernel<T, W><<<(unsigned)(((int64_t)a.batch * a.heads * a.q_rows + 3) / 4), 256, 0, st>>>(a);
 }
 
 template <typename T>
-void attention_by_width(const AttentionArgs& a, const AttentionPlan& plan, bool direct, hipStream_t st) {
+void attention_by_width(const AttentionArgs& a, bool direct, hipStream_t st) {
   switch (attention_width(a.head_dim)) {
-    case 64: attention_of<T, 64>(a, plan, direct, st); break;
-    case 96: attention_of<T, 96>(a, plan, direct, st); break;
-    case 128: attention_of<T, 128>(a, plan, direct, st); break;
-    default: attention_of<T, 256>(a, plan, direct, st); break;
+    case 64: attention_of<T, 64>(a, direct, st); break;
+    case 96: attention_of<T, 96>(a, direct, st); break;
+    case 128: attention_of<T, 128>(a, direct, st); break;
+    default: attention_of<T, 256>(a, direct, st); break;
   }
 }
 
@@ -476,8 +627,8 @@ int32_t launch_attention(const svdc_attention& p, const void* Q, const void* K, 
   const AttentionArgs a{Q, K, V, Out, reinterpret_cast<const int2*>(q_span), reinterpret_cast<const int2*>(k_span), key_mask,
                         static_cast<float*>(workspace), reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + (plan.parts > 1 ? sums_bytes(p, plan) : 0)),
                         p.q_total, p.k_total, p.q, p.k, p.v, p.o, (int)p.batch, p.heads, p.heads / p.kv_heads, p.head_dim, (int)p.q_rows, (int)p.k_rows,
-                        (int)((p.q_rows + 32 * plan.waves - 1) / (32 * plan.waves)), plan.parts, plan.tiles_of_part, p.scale * 1.4426950408889634f};
-  p.dtype == SVDC_F32 ? attention_by_width<float>(a, plan, direct, st) : attention_by_width<bf16_t>(a, plan, direct, st);
+                        (int)((p.q_rows + kTileQueries - 1) / kTileQueries), plan.parts, plan.tiles_of_part, p.scale * 1.4426950408889634f};
+  p.dtype == SVDC_F32 ? attention_by_width<float>(a, direct, st) : attention_by_width<bf16_t>(a, direct, st);
   return launch_status();
 }
 

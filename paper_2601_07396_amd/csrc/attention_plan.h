@@ -14,18 +14,19 @@ constexpr int attention_width(int head_dim) { return head_dim <= 64 ? 64 : head_
 // Keys that a workgroup takes at a time: 32 rows of S a matrix instruction, two of them where the registers allow it.
 constexpr int attention_tile_keys(int width, bool f32) { return !f32 && width <= 128 ? 64 : 32; }
 
-// waves of a workgroup, 32 queries each; parts of the keys, each a workgroup's, and the tiles of keys of a part
+constexpr int kTileQueries = 128;      // that a workgroup has, 32 a wave
+
+// parts of the keys, each a workgroup's, and the tiles of keys of a part
 struct AttentionPlan {
-  int waves, parts, tiles_of_part;
+  int parts, tiles_of_part;
 };
 
 inline AttentionPlan attention_plan(const svdc_attention& p, int cus) {
   const bool f32 = p.dtype == SVDC_F32;
   const int width = attention_width(p.head_dim), keys = attention_tile_keys(width, f32);
   AttentionPlan plan{};
-  plan.waves = width == 256 || p.q_rows <= 128 ? 4 : 8;
   const int64_t tiles = std::max<int64_t>(1, (p.k_rows + keys - 1) / keys);
-  const int64_t groups = p.batch * p.heads * ((p.q_rows + 32 * plan.waves - 1) / (32 * plan.waves));
+  const int64_t groups = p.batch * p.heads * ((p.q_rows + kTileQueries - 1) / kTileQueries);
   int64_t parts = 1;
   // parts of at least four tiles, until every compute unit has a workgroup or two
   if (groups > 0 && groups < cus) parts = std::min<int64_t>(std::min<int64_t>(2 * cus / groups, 64), (tiles + 3) / 4);

@@ -203,7 +203,7 @@ __device__ __forceinline__ float group_sum(float v) {
 template <typename TI, typename TO, int G, Columns C>
 __global__ __launch_bounds__(256) void norm_rotate_kernel(HeadsArgs a, int layout) {
   constexpr int EACH = kWave / G, AT_ONCE = 3;
-  const int wave = threadIdx.x / kWave, in_wave = threadIdx.x % kWave, mine = in_wave / G;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), in_wave = threadIdx.x % kWave, mine = in_wave / G;
   const Lane<G, C> lane(a, in_wave % G, layout == SVDC_PAIRS_HALVES);
   const int turns_q = a.q ? (a.heads + EACH - 1) / EACH : 0, turns_k = a.k ? (a.kv_heads + EACH - 1) / EACH : 0,
             turns = turns_q + turns_k + (a.v ? (a.kv_heads + EACH - 1) / EACH : 0);
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(HeadsArgs a, int layou
   lane.each([&](int t, int j, int, int) { turned[t] = j < a.pairs; });
   const float share = 1.f / (float)a.head_dim;
   for (int64_t at = blockIdx.x; at < a.all_rows; at += gridDim.x) {
-    const int b = (int)((uint32_t)at / (uint32_t)a.rows), row = (int)((uint32_t)at % (uint32_t)a.rows);
+    const int b = __builtin_amdgcn_readfirstlane((uint32_t)at / (uint32_t)a.rows), row = (int)at - b * a.rows;
     float2 turn_by[4];
     {
       const float2* table = reinterpret_cast<const float2*>(a.table) + (b * a.table_seq + (int64_t)row * a.pairs);
@@ -228,20 +228,21 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(HeadsArgs a, int layou
     }
     for (int turn0 = wave; turn0 < turns; turn0 += 4 * AT_ONCE) {
       float v[AT_ONCE][8];
-      // part and head of a turn; none beyond the last
-      const auto head_of = [&](int i, int& part) {
+      // part and head of a turn, the first of its heads; none beyond the last
+      const auto head_of = [&](int i, int& part, int& first) {
         int turn = turn0 + 4 * i;
         part = turn < turns_q ? 0 : turn < turns_q + turns_k ? 1 : 2;
         turn -= part == 0 ? 0 : part == 1 ? turns_q : turns_q + turns_k;
-        const int head = turn * EACH + mine;
+        first = turn * EACH;
+        const int head = first + mine;
         return turn0 + 4 * i < turns && head < (part ? a.kv_heads : a.heads) ? head : -1;
       };
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
-        int part;
-        const int head = head_of(i, part);
+        int part, first;
+        const int head = head_of(i, part, first);
         const svdc_heads& s = part == 0 ? a.sq : part == 1 ? a.sk : a.sv;
-        const TI* p = static_cast<const TI*>(part == 0 ? a.q : part == 1 ? a.k : a.v) + (b * s.seq + row * s.row + head * s.head);
+        const TI* p = static_cast<const TI*>(part == 0 ? a.q : part == 1 ? a.k : a.v) + (b * s.seq + row * s.row + first * s.head) + mine * s.head;
         if (head >= 0) {
           lane.load(p, v[i]);
         } else {
@@ -251,8 +252,8 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(HeadsArgs a, int layou
       }
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
-        int part;
-        const int head = head_of(i, part);
+        int part, first;
+        const int head = head_of(i, part, first);
         if (part < 2) {                                        // the same for all lanes
           if (a.norm) {
             float sum = 0.f;
@@ -272,7 +273,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(HeadsArgs a, int layou
           }
         }
         const svdc_heads& s = part == 0 ? a.sqo : part == 1 ? a.sko : a.svo;
-        TO* p = static_cast<TO*>(part == 0 ? a.qo : part == 1 ? a.ko : a.vo) + (b * s.seq + row * s.row + head * s.head);
+        TO* p = static_cast<TO*>(part == 0 ? a.qo : part == 1 ? a.ko : a.vo) + (b * s.seq + row * s.row + first * s.head) + mine * s.head;
         if (head >= 0) lane.store(p, v[i]);
       }
     }
