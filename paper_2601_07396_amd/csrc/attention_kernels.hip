@@ -27,10 +27,10 @@ struct AttentionArgs {
   void* Out;
   const int2 *q_span, *k_span;
   const uint8_t* mask;
-  float *sums, *stats;               // of parts: [batch][heads][part][q_rows][width] and [..][2]: maximum (times scale log2 e) and sum
+  float *sums, *stats;               // of parts: [unit][part][query][width] and [..][2]: what was subtracted from the exponents, and their powers' sum
   int64_t q_total, k_total;
   svdc_heads q, k, v, o;
-  int batch, heads, share, head_dim, q_rows, k_rows, q_tiles, parts, tiles_of_part;
+  int batch, heads, share, head_dim, q_rows, k_rows, q_tiles, whole, units, parts, tiles_of_part;
   float scale;                       // times log2 e
 };
 
@@ -42,6 +42,21 @@ __device__ __forceinline__ T* uniform(T* p) {
   return reinterpret_cast<T*>((uint64_t)(uint32_t)uniform((int)(u >> 32)) << 32 | (uint32_t)uniform((int)u));
 }
 
+// A unit of work: a head's tile of queries.  Workgroups go round the eight dies in turn, so with eight heads side by side, then the next rows of these heads, a die has a head at a time,
+// whose keys its workgroups share in the die's cache; and packed sequences of different lengths are spread over all dies (5 sequences of 0 to 1301 rows, 16 float32 heads:
+// 186 us; with a run of units for each die 415 us, which for equal lengths takes as long).
+struct Unit {
+  static constexpr int HEADS_AT_ONCE = 8;
+  int b, head, q_tile;
+  __device__ __forceinline__ Unit(const AttentionArgs& a, int id) {
+    b = uniform(id / (a.q_tiles * a.heads));
+    id -= b * a.q_tiles * a.heads;
+    const int first = id / (a.q_tiles * HEADS_AT_ONCE) * HEADS_AT_ONCE, side = min(HEADS_AT_ONCE, a.heads - first);
+    id -= first * a.q_tiles;
+    head = uniform(first + id % side);
+    q_tile = uniform(id / side);
+  }
+};
 // Rows of sequence b: the span's, as far as it lies within `total` rows, at most `most`
 struct Rows {
   int64_t first;
@@ -143,29 +158,20 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
   static_assert(LOADS * 64 * WAVES == KEYS * PITCH, "");
   __shared__ Lds<G::BYTES> columns0, columns1, keys0, keys1;  // two stages of values and of keys
 
-  constexpr int HEADS_AT_ONCE = 8;
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
-  // Workgroups go round the eight dies in turn; each die gets a run of them, HEADS_AT_ONCE heads side by side and then the next rows of these heads: the ones at work on
-  // a die at a time share keys in its cache, and where heads lie side by side in a row they do not all ask the same of its channels.
-  int q_tile, part, head, b;
-  {
-    const int all = gridDim.x, each = all / 8, more = all % 8, die = blockIdx.x % 8, of_head = a.q_tiles * a.parts;
-    int id = die * each + min(die, more) + blockIdx.x / 8;
-    b = uniform(id / (of_head * a.heads));
-    id -= b * of_head * a.heads;
-    const int first = id / (of_head * HEADS_AT_ONCE) * HEADS_AT_ONCE, side = min(HEADS_AT_ONCE, a.heads - first);
-    id -= first * of_head;
-    head = uniform(first + id % side);
-    q_tile = uniform(id / side % a.q_tiles);
-    part = uniform(id / side / a.q_tiles);
-  }
+  // The first `whole` workgroups have a unit each, the others a part of the keys of one of the rest.
+  const bool split = blockIdx.x >= (unsigned)a.whole;
+  const int at = blockIdx.x - (split ? a.whole : 0), rest = a.units - a.whole;
+  const int part = uniform(split ? at / rest : 0), unit = uniform(split ? a.whole + at % rest : at);
+  const Unit u(a, unit);
+  const int q_tile = u.q_tile, head = u.head, b = u.b;
   const Rows queries(a.q_span, b, a.q_total, a.q_rows), keys(a.k_span, b, a.k_total, a.k_rows);
   const int q0 = q_tile * kTileQueries;
   if (q0 >= queries.count) return;
   const int mine = q0 + 32 * wave + r;                        // this lane's query
   const bool there = mine < queries.count;
   const int k_count = uniform(keys.count);
-  const int from = uniform(part * a.tiles_of_part), to = uniform(min(from + a.tiles_of_part, (k_count + KEYS - 1) / KEYS));
+  const int from = uniform(part * a.tiles_of_part), to = uniform(min(split ? from + a.tiles_of_part : INT32_MAX, (k_count + KEYS - 1) / KEYS));
 
   const int kv_head = uniform(head / a.share);
   const T* K = uniform(static_cast<const T*>(a.K) + ((a.k_span ? 0 : b * a.k.seq) + keys.first * a.k.row + kv_head * a.k.head));
@@ -276,9 +282,19 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
   constexpr int STEPS = W / (2 * E);                          // 16 bytes of a row for each half of the wave
   u32x4 q[STEPS];
   {
-    const T* Q = static_cast<const T*>(a.Q) + ((a.q_span ? 0 : b * a.q.seq) + (queries.first + (there ? mine : 0)) * a.q.row + head * a.q.head);
+    const T* Q = static_cast<const T*>(a.Q) + ((a.q_span ? 0 : b * a.q.seq) + (queries.first + q0) * a.q.row + head * a.q.head);
+    if (DIRECT) {                                             // all at once, zeros for rows and columns that are not there
+      const int rows = min(kTileQueries, queries.count - q0), bytes = (int)(a.q.row * sizeof(T));
+      const auto from_here = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(uniform(Q)), 0, uniform((rows - 1) * bytes + row_bytes), 0x00027000);
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) q[s] = chunk_of(Q, 0, 0, 2 * s + h, 1);
+      for (int s = 0; s < STEPS; ++s) {
+        const uint32_t at = there && (2 * s + h) * 16 < row_bytes ? (uint32_t)((32 * wave + r) * bytes + (2 * s + h) * 16) : 0x80000000u;
+        q[s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_here, at, 0, 0));
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) q[s] = chunk_of(Q, a.q.row, there ? 32 * wave + r : 0, 2 * s + h, kTileQueries);
+    }
   }
 
   f32x16 o[W / 32] = {};
@@ -459,6 +475,21 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
       __syncthreads();
   };
 
+  if (DIRECT && q0 + 32 * wave >= queries.count) {
+    // a wave without queries loads its share of the tiles
+    if (from < to) begin();
+    for (int tile = from; tile + 1 < to; ++tile) {
+      begin();
+      keep[3] = present(tile + 3, byte);
+      byte = mask_byte(tile + 4);
+      fetch_values(tile + 1, keep[1], values_at(first + tile - from + 1));
+      fetch_keys(tile + 2, keep[2], keys_at(first + tile - from));
+#pragma unroll
+      for (int i = 0; i < 3; ++i) keep[i] = keep[i + 1];
+    }
+    if (from < to) begin();
+    return;
+  }
   if (from < to) {
     begin();
     first_keys(keys_at(first));
@@ -518,8 +549,8 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
     sum = lost | __shfl_xor(lost, 32) ? NAN : lane & 16 ? y : x;
   }
   if (!there) return;
-  if (a.parts > 1) {
-    const int64_t at = (((int64_t)b * a.heads + head) * a.parts + part) * a.q_rows + mine;
+  if (split) {
+    const int64_t at = ((int64_t)(unit - a.whole) * a.parts + part) * kTileQueries + 32 * wave + r;
     if (h == 0) {
       a.stats[2 * at] = sum == 0.f ? -INFINITY : fmaxf(shift, -3.4e38f);   // a sum that is no number counts
       a.stats[2 * at + 1] = sum;
@@ -545,24 +576,24 @@ __global__ __launch_bounds__(64 * WAVES, W <= 128 && DIRECT ? 2 : 1) void attent
 #endif
 }
 
-// Joins the parts of the keys, a wave for each query and head: lane l's columns are l, l + 64, ...
+// Joins the parts of the keys, a wave for each query of the units that were split: lane l's columns are l, l + 64, ...
 template <typename T, int W>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   const int lane = threadIdx.x % kWave;
-  const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;                 // (batch, head, row)
-  const int row = (int)(id % a.q_rows), head = (int)(id / a.q_rows % a.heads), b = (int)(id / ((int64_t)a.q_rows * a.heads));
-  if (b >= a.batch) return;
-  const Rows queries(a.q_span, b, a.q_total, a.q_rows);
+  const int id = uniform(blockIdx.x * 4 + threadIdx.x / kWave), n = id / kTileQueries, i = id % kTileQueries;
+  const Unit u(a, a.whole + n);
+  const Rows queries(a.q_span, u.b, a.q_total, a.q_rows);
+  const int row = u.q_tile * kTileQueries + i;
   if (row >= queries.count) return;
-  const int64_t first = ((int64_t)b * a.heads + head) * a.parts * a.q_rows + row;
+  const int64_t first = (int64_t)n * a.parts * kTileQueries + i;
   float top = -INFINITY, sum = 0.f;                            // of part `lane`
   if (lane < a.parts) {
-    const float2 s = reinterpret_cast<const float2*>(a.stats)[first + (int64_t)lane * a.q_rows];
+    const float2 s = reinterpret_cast<const float2*>(a.stats)[first + lane * kTileQueries];
     top = s.x, sum = s.y;
   }
   float high = top;
 #pragma unroll
-  for (int i = 32; i > 0; i >>= 1) high = fmaxf(high, __shfl_xor(high, i));
+  for (int e = 32; e > 0; e >>= 1) high = fmaxf(high, __shfl_xor(high, e));
   const float weight = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - high);
   const float total = wave_sum(top == -INFINITY ? 0.f : weight * sum);
   constexpr int EACH = (W + 63) / 64;
@@ -572,10 +603,10 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
     if (w == 0.f) continue;
 #pragma unroll
     for (int e = 0; e < EACH; ++e)
-      if (64 * e + lane < W) o[e] = __builtin_fmaf(w, a.sums[(first + (int64_t)p * a.q_rows) * W + 64 * e + lane], o[e]);
+      if (64 * e + lane < W) o[e] = __builtin_fmaf(w, a.sums[(first + p * kTileQueries) * W + 64 * e + lane], o[e]);
   }
   const float share = total == 0.f ? 0.f : 1.f / total;
-  T* Out = static_cast<T*>(a.Out) + ((a.q_span ? 0 : b * a.o.seq) + (queries.first + row) * a.o.row + head * a.o.head);
+  T* Out = static_cast<T*>(a.Out) + ((a.q_span ? 0 : u.b * a.o.seq) + (queries.first + row) * a.o.row + u.head * a.o.head);
 #pragma unroll
   for (int e = 0; e < EACH; ++e)
     if (64 * e + lane < a.head_dim) st_elem(Out, 64 * e + lane, o[e] * share);
@@ -588,9 +619,10 @@ void attention_masked(const AttentionArgs& a, unsigned grid, hipStream_t st) {
 
 template <typename T, int W>
 void attention_of(const AttentionArgs& a, bool direct, hipStream_t st) {
-  const unsigned grid = (unsigned)((int64_t)a.batch * a.heads * a.q_tiles * a.parts);
+  const int rest = a.units - a.whole;
+  const unsigned grid = (unsigned)(a.whole + rest * a.parts);
   direct ? attention_masked<T, W, true>(a, grid, st) : attention_masked<T, W, false>(a, grid, st);
-  if (a.parts > 1) attention_join_kernel<T, W><<<(unsigned)(((int64_t)a.batch * a.heads * a.q_rows + 3) / 4), 256, 0, st>>>(a);
+  if (rest) attention_join_kernel<T, W><<<rest * (kTileQueries / 4), 256, 0, st>>>(a);
 }
 
 template <typename T>
@@ -605,15 +637,15 @@ void attention_by_width(const AttentionArgs& a, bool direct, hipStream_t st) {
 
 // bytes of the parts' sums, a multiple of 256, and of their statistics
 size_t sums_bytes(const svdc_attention& p, const AttentionPlan& plan) {
-  return (size_t)p.batch * p.heads * plan.parts * p.q_rows * attention_width(p.head_dim) * sizeof(float);
+  return (size_t)(plan.units - plan.whole) * plan.parts * kTileQueries * attention_width(p.head_dim) * sizeof(float);
 }
-size_t stats_bytes(const svdc_attention& p, const AttentionPlan& plan) { return (size_t)p.batch * p.heads * plan.parts * p.q_rows * 2 * sizeof(float); }
+size_t stats_bytes(const AttentionPlan& plan) { return (size_t)(plan.units - plan.whole) * plan.parts * kTileQueries * 2 * sizeof(float); }
 
 }  // namespace
 
 size_t attention_workspace_bytes(const svdc_attention& p) {
   const AttentionPlan plan = attention_plan(p, num_compute_units());
-  return plan.parts > 1 ? sums_bytes(p, plan) + stats_bytes(p, plan) : 0;
+  return sums_bytes(p, plan) + stats_bytes(plan);
 }
 
 int32_t launch_attention(const svdc_attention& p, const void* Q, const void* K, const void* V, const int32_t* q_span, const int32_t* k_span,
@@ -623,11 +655,11 @@ int32_t launch_attention(const svdc_attention& p, const void* Q, const void* K, 
   const auto sixteen = [&](const void* x, const svdc_heads& s, bool spans) {
     return reinterpret_cast<uintptr_t>(x) % 16 == 0 && s.row % unit == 0 && s.head % unit == 0 && (spans || s.seq % unit == 0);
   };
-  const bool direct = p.head_dim % unit == 0 && sixteen(K, p.k, k_span) && sixteen(V, p.v, k_span);
+  const bool direct = p.head_dim % unit == 0 && sixteen(Q, p.q, q_span) && sixteen(K, p.k, k_span) && sixteen(V, p.v, k_span);
   const AttentionArgs a{Q, K, V, Out, reinterpret_cast<const int2*>(q_span), reinterpret_cast<const int2*>(k_span), key_mask,
-                        static_cast<float*>(workspace), reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + (plan.parts > 1 ? sums_bytes(p, plan) : 0)),
+                        static_cast<float*>(workspace), reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + sums_bytes(p, plan)),
                         p.q_total, p.k_total, p.q, p.k, p.v, p.o, (int)p.batch, p.heads, p.heads / p.kv_heads, p.head_dim, (int)p.q_rows, (int)p.k_rows,
-                        (int)((p.q_rows + kTileQueries - 1) / kTileQueries), plan.parts, plan.tiles_of_part, p.scale * 1.4426950408889634f};
+                        plan.q_tiles, plan.whole, plan.units, plan.parts, plan.tiles_of_part, p.scale * 1.4426950408889634f};
   p.dtype == SVDC_F32 ? attention_by_width<float>(a, direct, st) : attention_by_width<bf16_t>(a, direct, st);
   return launch_status();
 }

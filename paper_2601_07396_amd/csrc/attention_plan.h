@@ -15,23 +15,45 @@ constexpr int attention_width(int head_dim) { return head_dim <= 64 ? 64 : head_
 constexpr int attention_tile_keys(int width, bool f32) { return !f32 && width <= 128 ? 64 : 32; }
 
 constexpr int kTileQueries = 128;      // that a workgroup has, 32 a wave
+constexpr int kLeastTiles = 2;         // of a part
 
-// parts of the keys, each a workgroup's, and the tiles of keys of a part
+// Units of work are tiles of queries of a head: batch * heads * q_tiles.  The first `whole` of them are a workgroup's each, with all keys; each of the others is cut into `parts` parts of
+// tiles_of_part tiles of keys, a workgroup's each, which a second launch joins.  Without others parts is 1.
 struct AttentionPlan {
-  int parts, tiles_of_part;
+  int q_tiles, units, whole, parts, tiles_of_part;
 };
 
+constexpr int kMostParts = 64;         // a lane each when they are joined
+
 inline AttentionPlan attention_plan(const svdc_attention& p, int cus) {
-  const bool f32 = p.dtype == SVDC_F32;
-  const int width = attention_width(p.head_dim), keys = attention_tile_keys(width, f32);
+  const int width = attention_width(p.head_dim), keys = attention_tile_keys(width, p.dtype == SVDC_F32);
   AttentionPlan plan{};
+  plan.q_tiles = (int)((p.q_rows + kTileQueries - 1) / kTileQueries);
+  plan.units = (int)(p.batch * p.heads * plan.q_tiles);
+  plan.whole = plan.units;
+  plan.parts = 1;
   const int64_t tiles = std::max<int64_t>(1, (p.k_rows + keys - 1) / keys);
-  const int64_t groups = p.batch * p.heads * ((p.q_rows + kTileQueries - 1) / kTileQueries);
-  int64_t parts = 1;
-  // parts of at least four tiles, until every compute unit has a workgroup or two
-  if (groups > 0 && groups < cus) parts = std::min<int64_t>(std::min<int64_t>(2 * cus / groups, 64), (tiles + 3) / 4);
-  plan.tiles_of_part = (int)((tiles + parts - 1) / parts);
-  plan.parts = (int)((tiles + plan.tiles_of_part - 1) / plan.tiles_of_part);
+  const auto cut = [&](int whole, int64_t parts) {
+    plan.tiles_of_part = (int)((tiles + parts - 1) / parts);
+    plan.parts = (int)((tiles + plan.tiles_of_part - 1) / plan.tiles_of_part);
+    plan.whole = plan.parts > 1 ? whole : plan.units;
+  };
+  plan.tiles_of_part = (int)tiles;
+  const int rest = plan.units % cus;
+  if (plan.units > 0 && plan.units < cus) {
+    // fewer units than compute units: parts of all, until each of these has two workgroups
+    cut(0, std::min<int64_t>(std::min<int64_t>(std::max(1, 2 * cus / plan.units), kMostParts), (tiles + kLeastTiles - 1) / kLeastTiles));
+  } else if (rest) {
+    // The last round has work for some of the compute units only: its units in parts, if that takes less than what the parts' sums cost on their way through memory
+    const double round = tiles * keys * (width / 128.0) * (p.dtype == SVDC_F32 ? 0.075 : 0.0095), sums = 2.0 * kTileQueries * width * 4 / 4e6;
+    double least = round;
+    int64_t best = 1;
+    for (int64_t parts = 2; parts <= 8 && parts * kLeastTiles <= tiles; ++parts) {
+      const double us = round * (double)((rest * parts + cus - 1) / cus) / parts + rest * parts * sums + 5;
+      if (us < least) least = us, best = parts;
+    }
+    if (best > 1) cut(plan.units - rest, best);
+  }
   return plan;
 }
 

@@ -24,14 +24,14 @@ struct RotaryArgs {
   double theta[SVDC_MAX_AXES];
 };
 
-// cos and sin of 2 pi t.  t is reduced to an eighth of a turn around the next quarter in 64 bits, where nothing is lost; what is left has
-// 2^-28 of a turn of rounding as a float32.
+// cos and sin of 2 pi t.  t is reduced to an eighth of a turn around the next quarter in 64 bits, where nothing is lost; what is left, 2^-28 of a turn off as a
+// float32, goes into the first terms of the two Taylor series: at pi / 4 the next ones are 2^-29 (sine) and 2^-31 (cosine).
 __device__ __forceinline__ float2 turn(double t) {
-  const double quarter = rint(4.0 * t);
-  const float x = (float)(t - 0.25 * quarter);
-  float s, c;
-  sincospif(2.f * x, &s, &c);
-  const int q = (int)(quarter - 4.0 * floor(0.25 * quarter));
+  const double whole = t - rint(t), quarter = rint(4.0 * whole);
+  const float x = (float)__builtin_fma(quarter, -0.25, whole) * 6.2831853f, y = x * x;
+  const float s = x * __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, 2.7557319e-6f, -1.984127e-4f), 8.3333333e-3f), -0.16666667f), 1.f);
+  const float c = __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.f);
+  const int q = (int)quarter;
   const float2 half = q & 1 ? float2{-s, c} : float2{c, s};
   return q & 2 ? float2{-half.x, -half.y} : half;
 }
@@ -56,8 +56,18 @@ __global__ __launch_bounds__(256) void rotary_table_kernel(RotaryArgs a) {
   if (r >= rows_at_once) return;
   const double step = turns[j];
   const int axis = axis_of[j];
-  for (int64_t row = (int64_t)blockIdx.x * rows_at_once + r; row < a.rows; row += (int64_t)gridDim.x * rows_at_once)
-    reinterpret_cast<float2*>(a.table)[row * a.pairs + j] = turn((double)pos[row * a.ld + axis] * step);
+  const int64_t stride = (int64_t)gridDim.x * rows_at_once;
+  const T* from = pos + axis;
+  float2* to = reinterpret_cast<float2*>(a.table) + j;
+  int64_t row = (int64_t)blockIdx.x * rows_at_once + r;
+  for (; row + 3 * stride < a.rows; row += 4 * stride) {
+    T x[4];                                 // four rows' positions in flight
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = from[(row + i * stride) * a.ld];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to[(row + i * stride) * a.pairs] = turn((double)x[i] * step);
+  }
+  for (; row < a.rows; row += stride) to[row * a.pairs] = turn((double)from[row * a.ld] * step);
 }
 
 // ---- norm and rotation ------------------------------------------------------------------------------------------------
@@ -83,41 +93,24 @@ __device__ __forceinline__ void columns_of(int j, int pairs, bool halves, int& f
   to = split ? pairs + j : 2 * j + 1;
 }
 
-__device__ __forceinline__ float bits_of(const float* p) { return *p; }
-__device__ __forceinline__ float bits_of(const bf16_t* p) { return (float)*p; }
-
-// four columns in a row, at any alignment of an element
-__device__ __forceinline__ void load4(const bf16_t* p, float* v) {
-  typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-  const u32x2_any w = *reinterpret_cast<const u32x2_any*>(p);
-  v[0] = bf16_lo(w[0]), v[1] = bf16_hi(w[0]), v[2] = bf16_lo(w[1]), v[3] = bf16_hi(w[1]);
-}
-__device__ __forceinline__ void load4(const float* p, float* v) {
-  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-  const f32x4_any w = *reinterpret_cast<const f32x4_any*>(p);
+// four or eight columns in a row as they lie in memory, at any alignment of an element
+template <int N>
+__device__ __forceinline__ void load_words(const void* p, uint32_t* w) {
+  typedef uint32_t words __attribute__((ext_vector_type(N), aligned(2)));
+  const words x = *static_cast<const words*>(p);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = w[i];
+  for (int i = 0; i < N; ++i) w[i] = x[i];
 }
-__device__ __forceinline__ void load8(const bf16_t* p, float* v) {
-  const u32x4_any w = *reinterpret_cast<const u32x4_any*>(p);
+template <int N>
+__device__ __forceinline__ void store_words(void* p, const uint32_t* w) {
+  typedef uint32_t words __attribute__((ext_vector_type(N), aligned(2)));
+  words x;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[2 * i] = bf16_lo(w[i]), v[2 * i + 1] = bf16_hi(w[i]);
+  for (int i = 0; i < N; ++i) x[i] = w[i];
+  *static_cast<words*>(p) = x;
 }
-__device__ __forceinline__ void load8(const float* p, float* v) { load4(p, v), load4(p + 4, v + 4); }
-__device__ __forceinline__ void store4(bf16_t* p, const float* v) {
-  typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-  *reinterpret_cast<u32x2_any*>(p) = u32x2_any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-}
-__device__ __forceinline__ void store4(float* p, const float* v) {
-  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-  *reinterpret_cast<f32x4_any*>(p) = f32x4_any{v[0], v[1], v[2], v[3]};
-}
-__device__ __forceinline__ void store8(bf16_t* p, const float* v) {
-  *reinterpret_cast<u32x4_any*>(p) = u32x4_any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-}
-__device__ __forceinline__ void store8(float* p, const float* v) { store4(p, v), store4(p + 4, v + 4); }
 
-// A lane's columns of a head, v[2 t] and v[2 t + 1] the columns of its t-th pair
+// A lane's columns of a head, in the end v[2 t] and v[2 t + 1] the columns of its t-th pair
 template <int G, Columns C>
 struct Lane {
   int first;                // kNeighbours: its 8 columns; kHalves: its first four of either half, or its 8 columns behind them
@@ -130,7 +123,7 @@ struct Lane {
     split = C == kHalves && 4 * lane < pairs;
     if (split) first = 4 * lane;
   }
-  // what `f` makes of (pair t, its columns in v's order): for the tables and gains
+  // f(t, which of all pairs, its columns) for each of the lane's pairs
   template <typename F>
   __device__ __forceinline__ void each(F&& f) const {
 #pragma unroll
@@ -147,24 +140,39 @@ struct Lane {
       f(t, j, from, to);
     }
   }
+  // What lies in memory stays as it is until it is worked on: half the registers for bfloat16.
   template <typename T>
-  __device__ __forceinline__ void load(const T* p, float (&v)[8]) const {
+  static constexpr int words = C == kAnywhere ? 8 : 2 * (int)sizeof(T);
+  template <typename T>
+  __device__ __forceinline__ void load(const T* p, bool present, uint32_t (&w)[words<T>]) const {
+    constexpr int N = words<T>;
     if (C == kAnywhere) {
       each([&](int t, int, int from, int to) {
-        v[2 * t] = from < head_dim ? bits_of(p + from) : 0.f;
-        v[2 * t + 1] = to < head_dim ? bits_of(p + to) : 0.f;
+        w[2 * t] = __float_as_uint(present && from < head_dim ? ld_elem(p, from) : 0.f);
+        w[2 * t + 1] = __float_as_uint(present && to < head_dim ? ld_elem(p, to) : 0.f);
       });
-    } else if (!there) {
+    } else if (!(present && there)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+      for (int i = 0; i < N; ++i) w[i] = 0;
     } else if (C == kHalves && split) {
-      float lo[4], hi[4];
-      load4(p + first, lo);
-      load4(p + pairs + first, hi);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) v[2 * t] = lo[t], v[2 * t + 1] = hi[t];
+      load_words<N / 2>(p + first, w);
+      load_words<N / 2>(p + pairs + first, w + N / 2);
     } else {
-      load8(p + first, v);
+      load_words<4>(p + first, w);
+      if (N == 8) load_words<4>(reinterpret_cast<const uint32_t*>(p + first) + 4, w + N / 2);
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void unpack(const uint32_t (&w)[words<T>], float (&v)[8]) const {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      x[i] = C == kAnywhere || sizeof(T) == 4 ? __uint_as_float(w[i % words<T>]) : i % 2 ? bf16_hi(w[i / 2 % words<T>]) : bf16_lo(w[i / 2 % words<T>]);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const bool apart = C == kHalves && split;
+      v[2 * t] = apart ? x[t] : x[2 * t];
+      v[2 * t + 1] = apart ? x[4 + t] : x[2 * t + 1];
     }
   }
   template <typename T>
@@ -174,13 +182,23 @@ struct Lane {
         if (from < head_dim) st_elem(p, from, v[2 * t]);
         if (to < head_dim) st_elem(p, to, v[2 * t + 1]);
       });
-    } else if (!there) {
-    } else if (C == kHalves && split) {
-      const float lo[4] = {v[0], v[2], v[4], v[6]}, hi[4] = {v[1], v[3], v[5], v[7]};
-      store4(p + first, lo);
-      store4(p + pairs + first, hi);
+      return;
+    }
+    if (!there) return;
+    constexpr int N = 2 * (int)sizeof(T);
+    const bool apart = C == kHalves && split;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = apart ? v[2 * (i % 4) + i / 4] : v[i];
+    uint32_t w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = sizeof(T) == 4 ? __float_as_uint(x[i % 8]) : pack_bf16(x[2 * i % 8], x[(2 * i + 1) % 8]);
+    if (apart) {
+      store_words<N / 2>(p + first, w);
+      store_words<N / 2>(p + pairs + first, w + N / 2);
     } else {
-      store8(p + first, v);
+      store_words<4>(p + first, w);
+      if (N == 8) store_words<4>(reinterpret_cast<uint32_t*>(p + first) + 4, w + N / 2);
     }
   }
 };
@@ -198,92 +216,85 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// A workgroup takes a row at a time: G lanes a head, 64 / G heads a wave, the four waves the heads of Q, K and V in turn, AT_ONCE turns of loads in flight.
-// The gains stay in registers.
+// One of the three tensors.  A wave takes a row, G lanes a head, 64 / G heads at a time, AT_ONCE times that in flight; the table's part and the gain stay in registers.
 template <typename TI, typename TO, int G, Columns C>
-__global__ __launch_bounds__(256) void norm_rotate_kernel(HeadsArgs a, int layout) {
-  constexpr int EACH = kWave / G, AT_ONCE = 3;
+__device__ __forceinline__ void rows_of_heads(const HeadsArgs& a, const void* in, void* out, const svdc_heads& si, const svdc_heads& so, int heads, const float* gains, bool norm,
+                                              bool rotate, bool halves) {
+  constexpr int EACH = kWave / G, AT_ONCE = C == kAnywhere ? 2 : C == kHalves ? 3 : 6;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), in_wave = threadIdx.x % kWave, mine = in_wave / G;
-  const Lane<G, C> lane(a, in_wave % G, layout == SVDC_PAIRS_HALVES);
-  const int turns_q = a.q ? (a.heads + EACH - 1) / EACH : 0, turns_k = a.k ? (a.kv_heads + EACH - 1) / EACH : 0,
-            turns = turns_q + turns_k + (a.v ? (a.kv_heads + EACH - 1) / EACH : 0);
-  float gain[2][8];
-#pragma unroll
-  for (int part = 0; part < 2; ++part) {
-    const float* g = a.norm ? (part ? a.gain_k : a.gain_q) : nullptr;
-    lane.each([&](int t, int, int from, int to) {
-      gain[part][2 * t] = g && from < a.head_dim ? g[from] : 1.f;
-      gain[part][2 * t + 1] = g && to < a.head_dim ? g[to] : 1.f;
-    });
-  }
+  const Lane<G, C> lane(a, in_wave % G, halves);
+  float gain[8];
   bool turned[4];                 // what is not stays as it is, infinities beside it or not
-  lane.each([&](int t, int j, int, int) { turned[t] = j < a.pairs; });
+  lane.each([&](int t, int j, int from, int to) {
+    gain[2 * t] = gains && from < a.head_dim ? gains[from] : 1.f;
+    gain[2 * t + 1] = gains && to < a.head_dim ? gains[to] : 1.f;
+    turned[t] = rotate && j < a.pairs;
+  });
   const float share = 1.f / (float)a.head_dim;
-  for (int64_t at = blockIdx.x; at < a.all_rows; at += gridDim.x) {
+  const int64_t lane_in = mine * si.head, lane_out = mine * so.head;
+  for (int64_t at = (int64_t)blockIdx.x * 4 + wave; at < a.all_rows; at += (int64_t)gridDim.x * 4) {
     const int b = __builtin_amdgcn_readfirstlane((uint32_t)at / (uint32_t)a.rows), row = (int)at - b * a.rows;
+    const TI* from = static_cast<const TI*>(in) + (b * si.seq + row * si.row) + lane_in;
+    TO* to = static_cast<TO*>(out) + (b * so.seq + row * so.row) + lane_out;
     float2 turn_by[4];
-    {
-      const float2* table = reinterpret_cast<const float2*>(a.table) + (b * a.table_seq + (int64_t)row * a.pairs);
-      lane.each([&](int t, int j, int, int) { turn_by[t] = turned[t] ? table[j] : float2{1.f, 0.f}; });
-    }
-    for (int turn0 = wave; turn0 < turns; turn0 += 4 * AT_ONCE) {
-      float v[AT_ONCE][8];
-      // part and head of a turn, the first of its heads; none beyond the last
-      const auto head_of = [&](int i, int& part, int& first) {
-        int turn = turn0 + 4 * i;
-        part = turn < turns_q ? 0 : turn < turns_q + turns_k ? 1 : 2;
-        turn -= part == 0 ? 0 : part == 1 ? turns_q : turns_q + turns_k;
-        first = turn * EACH;
-        const int head = first + mine;
-        return turn0 + 4 * i < turns && head < (part ? a.kv_heads : a.heads) ? head : -1;
-      };
+    const float2* table = reinterpret_cast<const float2*>(a.table) + (b * a.table_seq + (int64_t)row * a.pairs);
+    lane.each([&](int t, int j, int, int) { turn_by[t] = turned[t] ? table[j] : float2{1.f, 0.f}; });
+    for (int head0 = 0; head0 < heads; head0 += AT_ONCE * EACH) {
+      uint32_t w[AT_ONCE][Lane<G, C>::template words<TI>];
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
-        int part, first;
-        const int head = head_of(i, part, first);
-        const svdc_heads& s = part == 0 ? a.sq : part == 1 ? a.sk : a.sv;
-        const TI* p = static_cast<const TI*>(part == 0 ? a.q : part == 1 ? a.k : a.v) + (b * s.seq + row * s.row + first * s.head) + mine * s.head;
-        if (head >= 0) {
-          lane.load(p, v[i]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-        }
+        const int head = head0 + i * EACH;
+        if (head < heads) lane.load(from + head * si.head, head + mine < heads, w[i]);
       }
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
-        int part, first;
-        const int head = head_of(i, part, first);
-        if (part < 2) {                                        // the same for all lanes
-          if (a.norm) {
-            float sum = 0.f;
+        const int head = head0 + i * EACH;
+        if (head >= heads) break;                              // for all lanes
+        float v[8];
+        lane.template unpack<TI>(w[i], v);
+        if (norm) {
+          float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(v[i][e], v[i][e], sum);
-            const float inv = 1.f / sqrtf(__builtin_fmaf(group_sum<G>(sum), share, a.eps));
+          for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(v[e], v[e], sum);
+          const float mean = __builtin_fmaf(group_sum<G>(sum), share, a.eps);
+          const float inv = __builtin_amdgcn_rsqf(mean < 1.17549435e-38f ? 1.17549435e-38f : mean);   // no number stays none
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * inv * (part ? gain[1][e] : gain[0][e]);
-          }
+          for (int e = 0; e < 8; ++e) v[e] = v[e] * inv * gain[e];
+        }
+        if (rotate) {
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            const float x = v[i][2 * t], y = v[i][2 * t + 1];
+            const float x = v[2 * t], y = v[2 * t + 1];
             if (turned[t]) {
-              v[i][2 * t] = __builtin_fmaf(x, turn_by[t].x, -(y * turn_by[t].y));
-              v[i][2 * t + 1] = __builtin_fmaf(x, turn_by[t].y, y * turn_by[t].x);
+              v[2 * t] = __builtin_fmaf(x, turn_by[t].x, -(y * turn_by[t].y));
+              v[2 * t + 1] = __builtin_fmaf(x, turn_by[t].y, y * turn_by[t].x);
             }
           }
         }
-        const svdc_heads& s = part == 0 ? a.sqo : part == 1 ? a.sko : a.svo;
-        TO* p = static_cast<TO*>(part == 0 ? a.qo : part == 1 ? a.ko : a.vo) + (b * s.seq + row * s.row + first * s.head) + mine * s.head;
-        if (head >= 0) lane.store(p, v[i]);
+        if (head + mine < heads) lane.store(to + head * so.head, v);
       }
     }
   }
 }
 
-// Workgroups for rows in turn: six to a compute unit keep it busy and read the gains seldom.
+// blockIdx.y: which of the tensors that are there
+template <typename TI, typename TO, int G, Columns C>
+__global__ __launch_bounds__(256, C == kAnywhere ? 3 : 4) void norm_rotate_kernel(HeadsArgs a, int layout) {
+  int part = blockIdx.y;
+  if (!a.q) ++part;
+  if (!a.k && part >= 1) ++part;
+  const bool halves = layout == SVDC_PAIRS_HALVES, rotate = a.pairs > 0;
+  if (part == 0)
+    rows_of_heads<TI, TO, G, C>(a, a.q, a.qo, a.sq, a.sqo, a.heads, a.norm ? a.gain_q : nullptr, a.norm, rotate, halves);
+  else if (part == 1)
+    rows_of_heads<TI, TO, G, C>(a, a.k, a.ko, a.sk, a.sko, a.kv_heads, a.norm ? a.gain_k : nullptr, a.norm, rotate, halves);
+  else
+    rows_of_heads<TI, TO, G, C>(a, a.v, a.vo, a.sv, a.svo, a.kv_heads, nullptr, false, false, halves);
+}
+
 template <typename TI, typename TO, int G>
 void norm_rotate_in(const HeadsArgs& a, int layout, hipStream_t st) {
-  const unsigned grid = (unsigned)std::min<int64_t>(a.all_rows, 6 * num_compute_units());
+  const dim3 grid((unsigned)std::min<int64_t>((a.all_rows + 3) / 4, 1 << 20), (a.q != nullptr) + (a.k != nullptr) + (a.v != nullptr));
   if (a.head_dim % 8 || a.pairs % 4)
     norm_rotate_kernel<TI, TO, G, kAnywhere><<<grid, 256, 0, st>>>(a, layout);
   else if (layout == SVDC_PAIRS_HALVES && a.pairs)

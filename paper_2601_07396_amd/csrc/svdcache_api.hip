@@ -69,7 +69,7 @@ int32_t check_attention(const svdc_attention* p, bool q_span, bool k_span) {
   if (p->batch > 65535 || !batch_rows_ok(p->batch, p->q_rows) || !batch_rows_ok(p->batch, p->k_rows) || p->heads < 1 || p->heads > kMaxHeads || p->kv_heads < 1 ||
       p->heads % p->kv_heads != 0 || p->head_dim < 1 || p->head_dim > kMaxHeadDim)
     return SVDC_E_SHAPE;
-  // workgroups of a launch, of 128 queries at least, and waves of the one that joins parts
+  // units of work, each at most 64 workgroups
   if (p->batch * p->heads * ((p->q_rows + 127) / 128) > (1 << 24)) return SVDC_E_SHAPE;
   if (q_span && (p->q_total < 0 || p->q_total > INT32_MAX)) return SVDC_E_SHAPE;
   if (k_span && (p->k_total < 0 || p->k_total > INT32_MAX)) return SVDC_E_SHAPE;
