@@ -221,39 +221,55 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
     for (int n = 0; n < LOADS; ++n) fetch(from_here, v_from[n], n, keep, stage);
   };
   // The same through registers, at any alignment and width.
-  const auto chunk_of = [&](const T* rows, int64_t row_stride, int row, int c, int count) INLINE {
+  // Heads of 16 bytes or more without branches, so that many loads are on their way: the chunk over a head's end is read as the head's last 16 bytes, and moved down when it is put
+  // to use.
+  const auto load_chunk = [&](const T* rows, int64_t row_stride, int row, int c, bool present) INLINE {
     u32x4 w = {};
     const int column = c * E;
-    if (row < count && column < a.head_dim) {
+    present = present && column < a.head_dim;
+    if (a.head_dim >= E) {
+      w = *reinterpret_cast<const u32x4_any*>(rows + (present ? row * row_stride + min(column, a.head_dim - E) : 0));
+    } else if (present) {
       const T* p = rows + row * row_stride + column;
-      if (column + E <= a.head_dim) {
-        w = *reinterpret_cast<const u32x4_any*>(p);
-      } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (column + e < a.head_dim) {
-            if (sizeof(T) == 4)
-              w[e] = reinterpret_cast<const uint32_t*>(p)[e];
-            else
-              w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << 16 * (e % 2);
-          }
-      }
+      for (int e = 0; e < E; ++e)
+        if (column + e < a.head_dim) {
+          if (sizeof(T) == 4)
+            w[e] = reinterpret_cast<const uint32_t*>(p)[e];
+          else
+            w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << 16 * (e % 2);
+        }
     }
     return w;
   };
+  const auto chunk_of = [&](u32x4 w, int c, bool present) INLINE {
+    const int over = a.head_dim >= E ? max(0, c * E + E - a.head_dim) : 0, bits = over * (int)sizeof(T) * 8;      // of columns behind the last one
+    const uint64_t lo = (uint64_t)w[1] << 32 | w[0], hi = (uint64_t)w[3] << 32 | w[2];
+    const uint64_t down_lo = bits >= 64 ? hi >> (bits & 63) : lo >> bits | (bits ? hi << (64 - bits) : 0), down_hi = bits >= 64 ? 0 : hi >> bits;
+    present = present && c * E < a.head_dim;
+    return present ? u32x4{(uint32_t)down_lo, (uint32_t)(down_lo >> 32), (uint32_t)down_hi, (uint32_t)(down_hi >> 32)} : u32x4{};
+  };
   const auto take = [&](const T* rows, int64_t stride, int tile, uint64_t keep, auto&& swizzle) INLINE {
+#pragma unroll
+    for (int n = 0; n < LOADS; ++n) kept[n] = u32x4{};
+    if (tile >= to) return;                                    // the first row of a tile that is there can be read
 #pragma unroll
     for (int n = 0; n < LOADS; ++n) {
       const int slot = (n * WAVES + wave) * 64 + lane, row = slot / PITCH, c = slot % PITCH;
-      kept[n] = chunk_of(rows + (int64_t)tile * KEYS * stride, stride, row, c ^ swizzle(row), tile < to && (keep >> row & 1) ? row + 1 : 0);
+      kept[n] = load_chunk(rows + (int64_t)tile * KEYS * stride, stride, row, c ^ swizzle(row), keep >> row & 1);
+    }
+  };
+  const auto put = [&](uint8_t* stage, uint64_t keep, auto&& swizzle) INLINE {
+#pragma unroll
+    for (int n = 0; n < LOADS; ++n) {
+      const int slot = (n * WAVES + wave) * 64 + lane, row = slot / PITCH, c = slot % PITCH;
+      *reinterpret_cast<u32x4*>(stage + slot * 16) = chunk_of(kept[n], c ^ swizzle(row), keep >> row & 1);
     }
   };
   const auto take_keys = [&](int tile, uint64_t keep) INLINE { take(K, a.k.row, tile, keep, G::key_swizzle); };
   const auto take_values = [&](int tile, uint64_t keep) INLINE { take(V, a.v.row, tile, keep, G::value_swizzle); };
-  const auto put = [&](uint8_t* stage) INLINE {
-#pragma unroll
-    for (int n = 0; n < LOADS; ++n) *reinterpret_cast<u32x4*>(stage + ((n * WAVES + wave) * 64 + lane) * 16) = kept[n];
-  };
+  const auto put_keys = [&](uint8_t* stage, uint64_t keep) INLINE { put(stage, keep, G::key_swizzle); };
+  const auto put_values = [&](uint8_t* stage, uint64_t keep) INLINE { put(stage, keep, G::value_swizzle); };
   // The last tile lies in stage 0.
   const int steps = max(0, to - from - 1), first = uniform(steps % 2);
   const auto keys_at = [&](int i) INLINE -> uint8_t* { return i % 2 ? keys1.b : keys0.b; };
@@ -272,9 +288,9 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
       fetch_keys(from + 1, keep[1], keys_at(first + 1));
       fetch_values(from, keep[0], values_at(first));
     } else {
-      take_keys(from, keep[0]), put(keys_at(first));
-      take_keys(from + 1, keep[1]), put(keys_at(first + 1));
-      take_values(from, keep[0]), put(values_at(first));
+      take_keys(from, keep[0]), put_keys(keys_at(first), keep[0]);
+      take_keys(from + 1, keep[1]), put_keys(keys_at(first + 1), keep[1]);
+      take_values(from, keep[0]), put_values(values_at(first), keep[0]);
     }
   }
 
@@ -293,7 +309,9 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
       }
     } else {
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) q[s] = chunk_of(Q, a.q.row, there ? 32 * wave + r : 0, 2 * s + h, kTileQueries);
+      for (int s = 0; s < STEPS; ++s) q[s] = load_chunk(Q, a.q.row, there ? 32 * wave + r : 0, 2 * s + h, true);
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) q[s] = chunk_of(q[s], 2 * s + h, true);
     }
   }
 
@@ -517,10 +535,10 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
       });
       first_values(values_now);
       follow(s);
-      if (!DIRECT) put(keys_now), take_values(tile + 1, keep[1]);
+      if (!DIRECT) put_keys(keys_now, keep[2]), take_values(tile + 1, keep[1]);
       if (keep[1] != ALL) leave_out(s_next, keep[1]);
       multiply_values(values_now);
-      if (!DIRECT) put(values_next);
+      if (!DIRECT) put_values(values_next, keep[1]);
 #pragma unroll
       for (int i = 0; i < 3; ++i) keep[i] = keep[i + 1];
     };

@@ -220,7 +220,7 @@ __device__ __forceinline__ float group_sum(float v) {
 template <typename TI, typename TO, int G, Columns C>
 __device__ __forceinline__ void rows_of_heads(const HeadsArgs& a, const void* in, void* out, const svdc_heads& si, const svdc_heads& so, int heads, const float* gains, bool norm,
                                               bool rotate, bool halves) {
-  constexpr int EACH = kWave / G, AT_ONCE = C == kAnywhere ? 2 : C == kHalves ? 3 : 6;
+  constexpr int EACH = kWave / G, AT_ONCE = C == kAnywhere ? 2 : C == kHalves ? 2 : 6;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), in_wave = threadIdx.x % kWave, mine = in_wave / G;
   const Lane<G, C> lane(a, in_wave % G, halves);
   float gain[8];
