@@ -480,12 +480,13 @@ int32_t svdcache_norm_rotate(const svdc_norm_rotate* p, const void* Q, const voi
 /* One attention. */
 typedef struct {
   int64_t batch;                 /* sequences, 0 .. 65535 */
-  int64_t q_rows, k_rows;        /* rows of a sequence, with spans the most that one has.  0 .. 2^31 - 1, batch times that as well */
-  int64_t q_total, k_total;      /* rows of Q and Out, of K and V, where spans say which of them a sequence has; else not read */
-  int32_t heads, kv_heads;       /* of Q and Out; of K and V: a divisor, each serves heads / kv_heads consecutive ones.  1 .. 2^16 */
+  int64_t q_rows, k_rows;        /* rows of a sequence, with spans the most that one has.  0 .. 2^30, batch times that at most 2^31 - 1 */
+  int64_t q_total, k_total;      /* rows of Q and Out, of K and V, where spans say which of them a sequence has (0 .. 2^31 - 1); else not read */
+  int32_t heads, kv_heads;       /* of Q and Out; of K and V: a divisor, each serves heads / kv_heads consecutive ones.  1 .. 2^16;
+                                    batch * heads * (q_rows / 128, rounded up) at most 2^24 */
   int32_t head_dim;              /* 1 .. 256 */
   int32_t dtype;                 /* svdc_dtype of all four: F32 or BF16 */
-  float scale;                   /* > 0, finite */
+  float scale;                   /* > 0, at most 1e38 */
   int32_t reserved;              /* set to 0 */
   svdc_heads q, k, v, o;         /* seq is not read where spans are given */
 } svdc_attention;

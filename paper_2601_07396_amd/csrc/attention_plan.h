@@ -45,7 +45,7 @@ inline AttentionPlan attention_plan(const svdc_attention& p, int cus) {
     cut(0, std::min<int64_t>(std::min<int64_t>(std::max(1, 2 * cus / plan.units), kMostParts), (tiles + kLeastTiles - 1) / kLeastTiles));
   } else if (rest) {
     // The last round has work for some of the compute units only: its units in parts, if that takes less than what the parts' sums cost on their way through memory
-    const double round = tiles * keys * (width / 128.0) * (p.dtype == SVDC_F32 ? 0.075 : 0.0095), sums = 2.0 * kTileQueries * width * 4 / 4e6;
+    const double round = tiles * keys * (width / 128.0) * (p.dtype == SVDC_F32 ? 0.115 : 0.0135), sums = 2.0 * kTileQueries * width * 4 / 4e6;
     double least = round;
     int64_t best = 1;
     for (int64_t parts = 2; parts <= 8 && parts * kLeastTiles <= tiles; ++parts) {

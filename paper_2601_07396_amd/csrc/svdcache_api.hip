@@ -53,7 +53,7 @@ int32_t check_matmul8(const svdc_matmul8* p) {
 
 // Limits of the operators around the attention.  With rows up to 2^31 and the strides' limits no offset leaves 2^62.
 constexpr int32_t kMaxHeadDim = 256, kMaxHeads = 1 << 16, kMaxTurned = 128;
-constexpr int64_t kMaxRowStride = int64_t(1) << 22, kMaxStride = int64_t(1) << 40;
+constexpr int64_t kMaxRowStride = int64_t(1) << 22, kMaxStride = int64_t(1) << 40, kMaxAttentionRows = int64_t(1) << 30;
 bool heads_ok(const svdc_heads& s, bool seq = true) {
   return s.row >= 0 && s.row <= kMaxRowStride && s.head >= 0 && s.head <= kMaxStride && (!seq || (s.seq >= 0 && s.seq <= kMaxStride));
 }
@@ -65,8 +65,8 @@ bool batch_rows_ok(int64_t batch, int64_t rows) {
 int32_t check_attention(const svdc_attention* p, bool q_span, bool k_span) {
   if (!p) return SVDC_E_NULL;
   if (!plain_dtype(p->dtype)) return SVDC_E_DTYPE;
-  if (!(p->scale > 0.f && p->scale <= 3.402823466e38f) || p->reserved != 0) return SVDC_E_PARAM;
-  if (p->batch > 65535 || !batch_rows_ok(p->batch, p->q_rows) || !batch_rows_ok(p->batch, p->k_rows) || p->heads < 1 || p->heads > kMaxHeads || p->kv_heads < 1 ||
+  if (!(p->scale > 0.f && p->scale <= 1e38f) || p->reserved != 0) return SVDC_E_PARAM;
+  if (p->batch > 65535 || p->q_rows > kMaxAttentionRows || p->k_rows > kMaxAttentionRows || !batch_rows_ok(p->batch, p->q_rows) || !batch_rows_ok(p->batch, p->k_rows) || p->heads < 1 || p->heads > kMaxHeads || p->kv_heads < 1 ||
       p->heads % p->kv_heads != 0 || p->head_dim < 1 || p->head_dim > kMaxHeadDim)
     return SVDC_E_SHAPE;
   // units of work, each at most 64 workgroups
