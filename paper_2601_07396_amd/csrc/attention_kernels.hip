@@ -341,7 +341,7 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
 
   // The products of a step are dealt out over the softmax's other work, so that both units are busy: `between(n, all)` does the n-th of `all` shares of it behind the n-th
   // product.
-  constexpr int AHEAD = W == 256 ? 1 : 3;                     // operands are read from LDS so many products ahead, as many as there are registers for
+  constexpr int AHEAD = G::F32 && W == 256 ? 1 : 3;                     // operands are read from LDS so many products ahead, as many as there are registers for
   constexpr int KEY_PRODUCTS = STEPS * BLOCKS, VALUE_PRODUCTS = G::F32 ? 16 * BLOCKS : 2 * BLOCKS * (W / 32);
   u32x4 k[AHEAD + 1];
   bf16x8 v[AHEAD + 1];

@@ -82,9 +82,10 @@ struct HeadsArgs {
   float eps;
 };
 
-// How the columns of a head lie in its lanes: 8 to a lane, as four pairs.  Anywhere: pairs lane, lane + G, ..., column by column.  The others want
-// head_dim in eights and turned pairs in fours, and load whole words: four pairs of neighbours are 8 columns in a row, of halves twice 4.
-enum Columns { kAnywhere, kNeighbours, kHalves };
+// How the columns of a head lie in its lanes: 8 to a lane, as four pairs.  Neighbours and halves want head_dim in eights and turned pairs in fours, and load whole words: four pairs
+// of neighbours are 8 columns in a row, of halves twice 4.  Odd ones are at home anywhere: pairs lane, lane + G, ..., a pair or a column at a time.
+enum Columns { kNeighbours, kHalves, kOddNeighbours, kOddHalves };
+constexpr bool odd_columns(Columns c) { return c == kOddNeighbours || c == kOddHalves; }
 
 // Pair `j` of all (turned ones first, then what is left by twos) -> its columns; `to` may be beyond the last column
 __device__ __forceinline__ void columns_of(int j, int pairs, bool halves, int& from, int& to) {
@@ -115,11 +116,11 @@ template <int G, Columns C>
 struct Lane {
   int first;                // kNeighbours: its 8 columns; kHalves: its first four of either half, or its 8 columns behind them
   int pairs, head_dim;
-  bool halves, split, there;
+  bool split, there;
 
-  __device__ __forceinline__ Lane(const HeadsArgs& a, int lane, bool halves) : pairs(a.pairs), head_dim(a.head_dim), halves(halves) {
-    first = C == kAnywhere ? lane : 8 * lane;
-    there = C == kAnywhere || first < head_dim;
+  __device__ __forceinline__ Lane(const HeadsArgs& a, int lane) : pairs(a.pairs), head_dim(a.head_dim) {
+    first = odd_columns(C) ? lane : 8 * lane;
+    there = odd_columns(C) || first < head_dim;
     split = C == kHalves && 4 * lane < pairs;
     if (split) first = 4 * lane;
   }
@@ -129,9 +130,9 @@ struct Lane {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       int j, from, to;
-      if (C == kAnywhere) {
+      if (odd_columns(C)) {
         j = first + t * G;
-        columns_of(j, pairs, halves, from, to);
+        columns_of(j, pairs, C == kOddHalves, from, to);
       } else if (C == kHalves && split) {
         j = from = first + t, to = pairs + from;
       } else {
@@ -142,14 +143,21 @@ struct Lane {
   }
   // What lies in memory stays as it is until it is worked on: half the registers for bfloat16.
   template <typename T>
-  static constexpr int words = C == kAnywhere ? 8 : 2 * (int)sizeof(T);
+  static constexpr int words = odd_columns(C) ? 8 : 2 * (int)sizeof(T);
   template <typename T>
   __device__ __forceinline__ void load(const T* p, bool present, uint32_t (&w)[words<T>]) const {
     constexpr int N = words<T>;
-    if (C == kAnywhere) {
+    if (odd_columns(C)) {
       each([&](int t, int, int from, int to) {
-        w[2 * t] = __float_as_uint(present && from < head_dim ? ld_elem(p, from) : 0.f);
-        w[2 * t + 1] = __float_as_uint(present && to < head_dim ? ld_elem(p, to) : 0.f);
+        if (C == kOddNeighbours && to < head_dim) {                 // two columns in a row
+          uint32_t both[2] = {};
+          if (present) load_words<(int)sizeof(T) / 2>(p + from, both);
+          w[2 * t] = sizeof(T) == 4 ? both[0] : both[0] << 16;
+          w[2 * t + 1] = sizeof(T) == 4 ? both[1] : both[0] & 0xffff0000u;
+        } else {
+          w[2 * t] = __float_as_uint(present && from < head_dim ? ld_elem(p, from) : 0.f);
+          w[2 * t + 1] = __float_as_uint(present && to < head_dim ? ld_elem(p, to) : 0.f);
+        }
       });
     } else if (!(present && there)) {
 #pragma unroll
@@ -167,7 +175,7 @@ struct Lane {
     float x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      x[i] = C == kAnywhere || sizeof(T) == 4 ? __uint_as_float(w[i % words<T>]) : i % 2 ? bf16_hi(w[i / 2 % words<T>]) : bf16_lo(w[i / 2 % words<T>]);
+      x[i] = odd_columns(C) || sizeof(T) == 4 ? __uint_as_float(w[i % words<T>]) : i % 2 ? bf16_hi(w[i / 2 % words<T>]) : bf16_lo(w[i / 2 % words<T>]);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const bool apart = C == kHalves && split;
@@ -177,10 +185,15 @@ struct Lane {
   }
   template <typename T>
   __device__ __forceinline__ void store(T* p, const float (&v)[8]) const {
-    if (C == kAnywhere) {
+    if (odd_columns(C)) {
       each([&](int t, int, int from, int to) {
-        if (from < head_dim) st_elem(p, from, v[2 * t]);
-        if (to < head_dim) st_elem(p, to, v[2 * t + 1]);
+        if (C == kOddNeighbours && to < head_dim) {
+          const uint32_t both[2] = {sizeof(T) == 4 ? __float_as_uint(v[2 * t]) : pack_bf16(v[2 * t], v[2 * t + 1]), __float_as_uint(v[2 * t + 1])};
+          store_words<(int)sizeof(T) / 2>(p + from, both);
+        } else {
+          if (from < head_dim) st_elem(p, from, v[2 * t]);
+          if (to < head_dim) st_elem(p, to, v[2 * t + 1]);
+        }
       });
       return;
     }
@@ -216,13 +229,14 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// One of the three tensors.  A wave takes a row, G lanes a head, 64 / G heads at a time, AT_ONCE times that in flight; the table's part and the gain stay in registers.
+// One of the three tensors.  A wave takes a row, G lanes a head, 64 / G heads at a time, AT_ONCE times that in flight, or as many rows of fewer heads; the table's part and the gain
+// stay in registers.
 template <typename TI, typename TO, int G, Columns C>
 __device__ __forceinline__ void rows_of_heads(const HeadsArgs& a, const void* in, void* out, const svdc_heads& si, const svdc_heads& so, int heads, const float* gains, bool norm,
-                                              bool rotate, bool halves) {
-  constexpr int EACH = kWave / G, AT_ONCE = C == kAnywhere ? 2 : C == kHalves ? 2 : 6;
+                                              bool rotate) {
+  constexpr int EACH = kWave / G, AT_ONCE = odd_columns(C) || C == kHalves ? 2 : G == 32 && sizeof(TI) == 4 ? 4 : 6;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), in_wave = threadIdx.x % kWave, mine = in_wave / G;
-  const Lane<G, C> lane(a, in_wave % G, halves);
+  const Lane<G, C> lane(a, in_wave % G);
   float gain[8];
   bool turned[4];                 // what is not stays as it is, infinities beside it or not
   lane.each([&](int t, int j, int from, int to) {
@@ -231,9 +245,11 @@ __device__ __forceinline__ void rows_of_heads(const HeadsArgs& a, const void* in
     turned[t] = rotate && j < a.pairs;
   });
   const float share = 1.f / (float)a.head_dim;
-  const int64_t lane_in = mine * si.head, lane_out = mine * so.head;
-  for (int64_t at = (int64_t)blockIdx.x * 4 + wave; at < a.all_rows; at += (int64_t)gridDim.x * 4) {
-    const int b = __builtin_amdgcn_readfirstlane((uint32_t)at / (uint32_t)a.rows), row = (int)at - b * a.rows;
+  const int rows_at_once = heads < EACH ? EACH / heads : 1, row_mine = heads < EACH ? mine / heads : 0, head_mine = heads < EACH ? mine % heads : mine;
+  const int64_t lane_in = head_mine * si.head, lane_out = head_mine * so.head;
+  for (int64_t at0 = ((int64_t)blockIdx.x * 4 + wave) * rows_at_once; at0 < a.all_rows; at0 += (int64_t)gridDim.x * 4 * rows_at_once) {
+    const bool here = row_mine < rows_at_once && at0 + row_mine < a.all_rows;
+    const int at = (int)(here ? at0 + row_mine : at0), b = a.all_rows == a.rows ? 0 : (int)((uint32_t)at / (uint32_t)a.rows), row = at - b * a.rows;
     const TI* from = static_cast<const TI*>(in) + (b * si.seq + row * si.row) + lane_in;
     TO* to = static_cast<TO*>(out) + (b * so.seq + row * so.row) + lane_out;
     float2 turn_by[4];
@@ -244,7 +260,7 @@ __device__ __forceinline__ void rows_of_heads(const HeadsArgs& a, const void* in
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
         const int head = head0 + i * EACH;
-        if (head < heads) lane.load(from + head * si.head, head + mine < heads, w[i]);
+        if (head < heads) lane.load(from + head * si.head, here && head + head_mine < heads, w[i]);
       }
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
@@ -271,7 +287,7 @@ __device__ __forceinline__ void rows_of_heads(const HeadsArgs& a, const void* in
             }
           }
         }
-        if (head + mine < heads) lane.store(to + head * so.head, v);
+        if (here && head + head_mine < heads) lane.store(to + head * so.head, v);
       }
     }
   }
@@ -279,28 +295,25 @@ __device__ __forceinline__ void rows_of_heads(const HeadsArgs& a, const void* in
 
 // blockIdx.y: which of the tensors that are there
 template <typename TI, typename TO, int G, Columns C>
-__global__ __launch_bounds__(256, C == kAnywhere ? 3 : 4) void norm_rotate_kernel(HeadsArgs a, int layout) {
+__global__ __launch_bounds__(256, odd_columns(C) ? 3 : 4) void norm_rotate_kernel(HeadsArgs a) {
   int part = blockIdx.y;
   if (!a.q) ++part;
   if (!a.k && part >= 1) ++part;
-  const bool halves = layout == SVDC_PAIRS_HALVES, rotate = a.pairs > 0;
-  if (part == 0)
-    rows_of_heads<TI, TO, G, C>(a, a.q, a.qo, a.sq, a.sqo, a.heads, a.norm ? a.gain_q : nullptr, a.norm, rotate, halves);
-  else if (part == 1)
-    rows_of_heads<TI, TO, G, C>(a, a.k, a.ko, a.sk, a.sko, a.kv_heads, a.norm ? a.gain_k : nullptr, a.norm, rotate, halves);
-  else
-    rows_of_heads<TI, TO, G, C>(a, a.v, a.vo, a.sv, a.svo, a.kv_heads, nullptr, false, false, halves);
+  const bool q = part == 0, k = part == 1;
+  rows_of_heads<TI, TO, G, C>(a, q ? a.q : k ? a.k : a.v, q ? a.qo : k ? a.ko : a.vo, q ? a.sq : k ? a.sk : a.sv, q ? a.sqo : k ? a.sko : a.svo, q ? a.heads : a.kv_heads,
+                              !a.norm ? nullptr : q ? a.gain_q : k ? a.gain_k : nullptr, a.norm && part < 2, a.pairs > 0 && part < 2);
 }
 
 template <typename TI, typename TO, int G>
 void norm_rotate_in(const HeadsArgs& a, int layout, hipStream_t st) {
-  const dim3 grid((unsigned)std::min<int64_t>((a.all_rows + 3) / 4, 1 << 20), (a.q != nullptr) + (a.k != nullptr) + (a.v != nullptr));
-  if (a.head_dim % 8 || a.pairs % 4)
-    norm_rotate_kernel<TI, TO, G, kAnywhere><<<grid, 256, 0, st>>>(a, layout);
-  else if (layout == SVDC_PAIRS_HALVES && a.pairs)
-    norm_rotate_kernel<TI, TO, G, kHalves><<<grid, 256, 0, st>>>(a, layout);
+  const auto waves = [&](int heads) { return (a.all_rows * std::min(heads, kWave / G) + kWave / G - 1) / (kWave / G); };      // about
+  const int64_t most = std::max(a.q ? waves(a.heads) : 0, a.k || a.v ? waves(a.kv_heads) : 0);
+  const dim3 grid((unsigned)std::min<int64_t>((most + 3) / 4, 1 << 20), (a.q != nullptr) + (a.k != nullptr) + (a.v != nullptr));
+  const bool halves = layout == SVDC_PAIRS_HALVES && a.pairs, odd = a.head_dim % 8 || a.pairs % 4;
+  if (odd)
+    halves ? norm_rotate_kernel<TI, TO, G, kOddHalves><<<grid, 256, 0, st>>>(a) : norm_rotate_kernel<TI, TO, G, kOddNeighbours><<<grid, 256, 0, st>>>(a);
   else
-    norm_rotate_kernel<TI, TO, G, kNeighbours><<<grid, 256, 0, st>>>(a, layout);
+    halves ? norm_rotate_kernel<TI, TO, G, kHalves><<<grid, 256, 0, st>>>(a) : norm_rotate_kernel<TI, TO, G, kNeighbours><<<grid, 256, 0, st>>>(a);
 }
 
 template <typename TI, typename TO>
