@@ -444,7 +444,7 @@ typedef struct {
 } svdc_rotary;
 
 /* table[row][j] = (cos, sin) of pos[row][a] * theta[a]^(-2 i / dims[a]) with pair j the i-th of axis a.  Angles are made and reduced in 64 bits:
- * positions as far as 2^31 lose nothing (an angle is off by at most 2^-51 of itself, cosine and sine by 2^-24 more).  A position that
+ * positions as far as 2^31 lose nothing (an angle is off by at most 2^-51 of itself, cosine and sine by less than 2^-22 more).  A position that
  * is not finite gives NaN.
  *   pos    in   [rows, axes] float32 or int32
  *   table  out  [rows, pairs, 2] float32, dense, 8-byte aligned, with pairs = sum of dims / 2 */
@@ -509,7 +509,7 @@ size_t svdcache_attention_workspace_bytes(const svdc_attention* p);
  *                  call until it has completed on the stream: calls in flight on different streams need one each.
  * Pointers are aligned to their elements; rows and heads at multiples of 16 bytes of one another (pointers, strides and head_dim) are read faster.
  * Products and sums, the softmax's maximum and sum are float32.  For bfloat16 the probabilities enter the second product rounded to
- * bfloat16, which is as much off as rounding the result is; float32 uses float32 products throughout.  Results do not depend on anything but the
+ * bfloat16, which is as much off as rounding the result is; float32 uses float32 products throughout.  The exponential is the hardware's power of two (a step of the last place).  Results do not depend on anything but the
  * arguments and the number of compute units (no atomics). */
 int32_t svdcache_attention(const svdc_attention* p, const void* Q, const void* K, const void* V, const int32_t* q_span, const int32_t* k_span,
                            const uint8_t* key_mask, void* Out, void* workspace, size_t workspace_bytes, void* stream);

@@ -41,10 +41,12 @@ inline AttentionPlan attention_plan(const svdc_attention& p, int cus) {
   plan.tiles_of_part = (int)tiles;
   const int rest = plan.units % cus;
   if (plan.units > 0 && plan.units < cus) {
-    // fewer units than compute units: parts of all, until each of these has two workgroups
+    // Fewer units than compute units: parts of all, until each of these has two workgroups.  64 x 119056, 24 heads: 21 parts 275 us (whole: 24 workgroups).  1 x 512, 24 heads: 4 parts
+    // 9.7 us, whole 10.5
     cut(0, std::min<int64_t>(std::min<int64_t>(std::max(1, 2 * cus / plan.units), kMostParts), (tiles + kLeastTiles - 1) / kLeastTiles));
   } else if (rest) {
-    // The last round has work for some of the compute units only: its units in parts, if that takes less than what the parts' sums cost on their way through memory
+    // The last round has work for some of the compute units only: its units in parts, if that takes less than what the parts' sums cost on their way through memory.
+    // 4608 x 4608, 24 heads, 864 units: the last 96 in 5 parts 246 us, whole 259; 4 sequences of it 949 and 965; 29764 x 29764, 3 heads 1.20 and 1.25 ms
     const double round = tiles * keys * (width / 128.0) * (p.dtype == SVDC_F32 ? 0.115 : 0.0135), sums = 2.0 * kTileQueries * width * 4 / 4e6;
     double least = round;
     int64_t best = 1;

@@ -1,7 +1,10 @@
 // Heads of queries and keys on their way into the attention: angles of a rotation with several position axes (svdcache_rotary_table), norm and
 // rotation of each head in one pass (svdcache_norm_rotate).
 //
-// Both stream their rows once and reuse next to nothing.
+// Both stream their rows once and reuse next to nothing.  Norm and rotation are bound by memory (a copy of 1 GiB reaches 5.2 TB/s):
+//     4608 rows, 24 + 24 heads of 128, bfloat16 (116 MB) 25.7 us, 4.5 TB/s, 21.9 of it in the kernel; 4 x 4096 rows, float32 into bfloat16 with values (908 MB) 172 us, 5.3 TB/s
+//     odd heads: 3 x 1001 rows, 16 + 8 heads of 72, 27 pairs of halves, float32 (42 MB) 12.7 us; one row 4.1 us, a launch
+// The angles are bound by their arithmetic in 64 bits: 119056 x 64 pairs (62 MB) 16 us, 3.9 TB/s; 4608 x 64 4.1 us.
 #include <algorithm>
 
 #include "eight_bit.h"
