@@ -486,11 +486,12 @@ int32_t svdcache_attention(const svdc_attention* p, const void* Q, const void* K
                            const uint8_t* key_mask, void* Out, void* workspace, size_t workspace_bytes, void* stream) {
   const int32_t rc = check_attention(p, q_span != nullptr, k_span != nullptr);
   if (rc != SVDC_OK) return rc;
-  if (p->batch == 0 || p->q_rows == 0) return SVDC_OK;
-  if (!Q || !Out || (p->k_rows && (!K || !V))) return SVDC_E_NULL;
+  if (p->batch == 0 || p->q_rows == 0 || (q_span && p->q_total == 0)) return SVDC_OK;
+  const bool keys = p->k_rows && !(k_span && p->k_total == 0);   // else results are zeros
+  if (!Q || !Out || (keys && (!K || !V))) return SVDC_E_NULL;
   const size_t unit = dtype_size(p->dtype);
   if (!aligned(Q, unit) || !aligned(K, unit) || !aligned(V, unit) || !aligned(Out, unit) || !aligned(q_span, 8) || !aligned(k_span, 8)) return SVDC_E_ALIGN;
-  if (Out == Q || (p->k_rows && (Out == K || Out == V))) return SVDC_E_PARAM;
+  if (Out == Q || (keys && (Out == K || Out == V))) return SVDC_E_PARAM;
   const size_t need = attention_workspace_bytes(*p);
   if (need && !workspace) return SVDC_E_NULL;
   if (need && !aligned(workspace, 256)) return SVDC_E_ALIGN;

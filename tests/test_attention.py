@@ -237,7 +237,32 @@ def test_no_rows_and_no_keys():
 
 
 @gpu
-@pytest.mark.parametrize("size", [(1, 300, 400, 2, 2, 128), (1, 4, 3000, 2, 2, 128)], ids=["whole", "parts"])
+def test_spans_of_nothing():
+    """Tensors without rows: nothing to write, or no keys for anybody."""
+    q, none = torch.ones(6, 3, 64, device="cuda"), torch.ones(0, 3, 64, device="cuda")
+    span, out = torch.tensor([[0, 4], [4, 9]], dtype=torch.int32, device="cuda"), torch.full((6, 3, 64), 7.0, device="cuda")
+    call(q, none, none, out, span, span, q_most=9, k_most=9)
+    assert (out == 0).all()
+    call(none, q, q, torch.empty_like(none), span, span, q_most=9, k_most=9)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,m", [(BF16, 4100), (BF16, 130), (F32, 2050)])
+def test_more_units_than_compute_units(dtype, m):
+    """360 units of work: a workgroup each for the first ones, parts of the keys for the last ones where there are many keys."""
+    batch, n, h, d = 3, 640, 24, 128
+    g = torch.Generator().manual_seed(15)
+    q, k, v = heads(g, batch, n, h, d, dtype), heads(g, batch, m, h, d, dtype), heads(g, batch, m, h, d, dtype)
+    out = like(q)
+    p = call(q, k, v, out)
+    assert (svdc.svdcache_attention_workspace_bytes(p) > 0) == (m > 1000)
+    assert torch.isfinite(out).all()
+    for b, head in ((0, 0), (1, 13), (2, 7), (2, 15), (2, 16), (2, 23)):
+        check(out[b][:, head:head + 1], q[b][:, head:head + 1], k[b][:, head:head + 1], v[b][:, head:head + 1], d ** -0.5, dtype)
+
+
+@gpu
+@pytest.mark.parametrize("size", [(1, 300, 400, 2, 2, 128), (1, 4, 3000, 2, 2, 128), (2, 700, 4100, 24, 24, 64)], ids=["whole", "parts", "last_round"])
 def test_streams_graphs_and_repeats(size):
     """The same bits on other streams at once (a workspace each), when repeated, and from a captured graph on new inputs with eager work in between."""
     batch, n, m, h, hk, d = size
@@ -321,6 +346,7 @@ def test_refused_pointers():
         assert status(p, **{name: 4 * POINTER}) == -5
     assert status(descriptor(q_total=-1), q_span=POINTER) == -2 and status(descriptor(k_total=2 ** 31), k_span=POINTER) == -2
     assert status(descriptor(batch=0), Q=0) == 0 and status(descriptor(q_rows=0), Q=0) == 0
+    assert status(descriptor(q_total=0), Q=0, q_span=POINTER) == 0
 
 
 def test_workspace_is_checked():

@@ -137,7 +137,7 @@ def inputs(batch, rows, heads, kv, d, pairs, dtype, per_seq=False, seed=2):
 @pytest.mark.parametrize("size", [  # batch, rows, heads, heads of keys, head_dim, pairs
     (1, 1, 24, 24, 128, 64), (2, 37, 5, 5, 128, 64), (1, 9, 16, 8, 72, 36), (1, 9, 16, 8, 72, 27), (3, 4, 7, 1, 64, 32), (1, 3, 3, 2, 64, 20), (1, 5, 2, 2, 256, 128),
     (1, 5, 2, 1, 256, 100), (1, 4, 3, 3, 33, 16), (1, 4, 3, 3, 33, 0), (2, 3, 2, 2, 1, 0), (1, 2, 50, 7, 8, 4), (1, 3, 2, 2, 130, 65), (1, 2, 2, 2, 24, 12),
-    (1, 2, 130, 3, 2, 1), (1, 700, 2, 2, 96, 48)], ids=lambda s: "x".join(map(str, s)))
+    (1, 2, 130, 3, 2, 1), (1, 700, 2, 2, 96, 48), (3, 531, 1, 3, 128, 64), (2, 301, 5, 1, 8, 4), (5, 67, 3, 2, 40, 18)], ids=lambda s: "x".join(map(str, s)))
 def test_heads(size, layout, dtype, dtype_out):
     batch, rows, heads, kv, d, pairs = size
     q, k, v, (gq, gk), table = inputs(batch, rows, heads, kv, d, pairs, dtype)
