@@ -622,14 +622,23 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   for (int e = 32; e > 0; e >>= 1) high = fmaxf(high, __shfl_xor(high, e));
   const float weight = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - high);
   const float total = wave_sum(top == -INFINITY ? 0.f : weight * sum);
-  constexpr int EACH = (W + 63) / 64;
+  constexpr int EACH = (W + 63) / 64, AT_ONCE = 8 / EACH;       // loads in flight
   float o[EACH] = {};
-  for (int p = 0; p < a.parts; ++p) {
-    const float w = __shfl(weight, p);
-    if (w == 0.f) continue;
+  const float* from = a.sums + first * W + lane;
+  for (int p0 = 0; p0 < a.parts; p0 += AT_ONCE) {
+    float x[AT_ONCE][EACH];
 #pragma unroll
-    for (int e = 0; e < EACH; ++e)
-      if (64 * e + lane < W) o[e] = __builtin_fmaf(w, a.sums[(first + p * kTileQueries) * W + 64 * e + lane], o[e]);
+    for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+      for (int e = 0; e < EACH; ++e)
+        if (64 * e + lane < W) x[i][e] = from[(int64_t)min(p0 + i, a.parts - 1) * kTileQueries * W + 64 * e];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const float w = __shfl(weight, (p0 + i) % kWave);        // 0 behind the last part and for one without keys, whose sums were not written
+#pragma unroll
+      for (int e = 0; e < EACH; ++e)
+        if (64 * e + lane < W && w != 0.f && p0 + i < a.parts) o[e] = __builtin_fmaf(w, x[i][e], o[e]);
+    }
   }
   const float share = total == 0.f ? 0.f : 1.f / total;
   T* Out = static_cast<T*>(a.Out) + ((a.q_span ? 0 : u.b * a.o.seq) + (queries.first + row) * a.o.row + u.head * a.o.head);
