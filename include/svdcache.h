@@ -483,7 +483,7 @@ typedef struct {
   int64_t q_rows, k_rows;        /* rows of a sequence, with spans the most that one has.  0 .. 2^30, batch times that at most 2^31 - 1 */
   int64_t q_total, k_total;      /* rows of Q and Out, of K and V, where spans say which of them a sequence has (0 .. 2^31 - 1); else not read */
   int32_t heads, kv_heads;       /* of Q and Out; of K and V: a divisor, each serves heads / kv_heads consecutive ones.  1 .. 2^16;
-                                    batch * heads * (q_rows / 128, rounded up) at most 2^24 */
+                                    batch * heads * (q_rows / 128, rounded up) at most 2^23 */
   int32_t head_dim;              /* 1 .. 256 */
   int32_t dtype;                 /* svdc_dtype of all four: F32 or BF16 */
   float scale;                   /* > 0, at most 1e38 */

@@ -8,10 +8,10 @@
 // P = 2^(scale log2(e) S - shift) is rounded to bfloat16 for bfloat16 tensors (the matrix cores' other operand, V, is that too): 2^-9 of each probability at random, as much as the
 // rounding of the result.  Its sums are made of the rounded numbers, so that what rounding moves the probabilities by on the whole drops out.
 //
-// What bounds it: the matrix cores, and the clock, which the card lowers under this load.  4608 x 4608, 24 heads of 128, bfloat16: 245 us, 1065 TFLOP/s; while every
+// What bounds it: the matrix cores, and the clock, which the card lowers under this load.  4608 x 4608, 24 heads of 128, bfloat16: 242 us, 1080 TFLOP/s; while every
 // compute unit has two workgroups its matrix cores are 84 % busy, at 1.7 GHz; over the whole call 59 % at 1.86 GHz.  A large bfloat16 matrix product reaches 1410 TFLOP/s on
 // the card.  29764 x 29764, 3 heads: 1.20 ms, 1135 TFLOP/s.  float32 products go at a sixteenth of the rate: 4608 x 4608, 24 heads, 1.84 ms, 142 TFLOP/s of 154.  Few rows are bound by
-// memory: 64 queries over 119056 keys of 24 heads 275 us, 5.3 TB/s.  Forms that were slower: eight waves of 32 queries with four stages, half of them half a step behind (255 us; 47 %
+// memory: 64 queries over 119056 keys of 24 heads 270 us, 5.4 TB/s.  Forms that were slower: eight waves of 32 queries with four stages, half of them half a step behind (255 us; 47 %
 // busy, one barrier for eight waves); the maximum of each tile before its exponentials (271 us); sums by additions beside the exponentials (they cost a sixth of that phase).
 #include <algorithm>
 #include <type_traits>
@@ -38,7 +38,7 @@ struct AttentionArgs {
   float *sums, *stats;               // of parts: [unit][part][query][width] and [..][2]: what was subtracted from the exponents, and their powers' sum
   int64_t q_total, k_total;
   svdc_heads q, k, v, o;
-  int batch, heads, share, head_dim, q_rows, k_rows, q_tiles, whole, units, parts, tiles_of_part;
+  int kv_heads, share, head_dim, q_rows, k_rows, q_tiles, whole, units, parts, tiles_of_part;
   float scale;                       // times log2 e
 };
 
@@ -50,21 +50,39 @@ __device__ __forceinline__ T* uniform(T* p) {
   return reinterpret_cast<T*>((uint64_t)(uint32_t)uniform((int)(u >> 32)) << 32 | (uint32_t)uniform((int)u));
 }
 
-// A unit of work: a head's tile of queries.  Workgroups go round the eight dies in turn, so with eight heads side by side, then the next rows of these heads, a die has a head at a time,
-// whose keys its workgroups share in the die's cache; and packed sequences of different lengths are spread over all dies (5 sequences of 0 to 1301 rows, 16 float32 heads:
-// 186 us; with a run of units for each die 415 us, which for equal lengths takes as long).
+// A unit of work: a tile of the queries of all heads that share a head of keys, one head's rows behind the other's.  Workgroups go round the eight dies in turn, so with eight heads of
+// keys side by side, then the next queries of these, a die has a head at a time, whose keys its workgroups share in the die's cache; and packed sequences of different lengths are
+// spread over all dies (5 sequences of 0 to 1301 rows, 16 float32 heads: 186 us; with a run of units for each die 415 us, which for equal lengths takes as long).
 struct Unit {
   static constexpr int HEADS_AT_ONCE = 8;
-  int b, head, q_tile;
+  int b, kv_head, q_tile;
   __device__ __forceinline__ Unit(const AttentionArgs& a, int id) {
-    b = uniform(id / (a.q_tiles * a.heads));
-    id -= b * a.q_tiles * a.heads;
-    const int first = id / (a.q_tiles * HEADS_AT_ONCE) * HEADS_AT_ONCE, side = min(HEADS_AT_ONCE, a.heads - first);
+    b = uniform(id / (a.q_tiles * a.kv_heads));
+    id -= b * a.q_tiles * a.kv_heads;
+    const int first = id / (a.q_tiles * HEADS_AT_ONCE) * HEADS_AT_ONCE, side = min(HEADS_AT_ONCE, a.kv_heads - first);
     id -= first * a.q_tiles;
-    head = uniform(first + id % side);
+    kv_head = uniform(first + id % side);
     q_tile = uniform(id / side);
   }
 };
+// Query i of a unit: its row of the sequence and its head, and where it lies in a tensor from the sequence's first row on
+struct Query {
+  int row, head;
+  bool there;
+  __device__ __forceinline__ Query(const AttentionArgs& a, const Unit& u, int i, int count) {
+    const int at = u.q_tile * kTileQueries + i;
+    if (a.share == 1) {                    // without a division
+      row = at, head = u.kv_head, there = row < count;
+    } else {
+      const int of_share = at / a.q_rows;
+      row = at - of_share * a.q_rows;
+      head = u.kv_head * a.share + of_share;
+      there = of_share < a.share && row < count;
+    }
+  }
+  __device__ __forceinline__ int64_t at(const svdc_heads& s, int64_t first) const { return (first + row) * s.row + head * s.head; }
+};
+
 // Rows of sequence b: the span's, as far as it lies within `total` rows, at most `most`
 struct Rows {
   int64_t first;
@@ -172,16 +190,16 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
   const int at = blockIdx.x - (split ? a.whole : 0), rest = a.units - a.whole;
   const int part = uniform(split ? at / rest : 0), unit = uniform(split ? a.whole + at % rest : at);
   const Unit u(a, unit);
-  const int q_tile = u.q_tile, head = u.head, b = u.b;
+  const int b = u.b, kv_head = u.kv_head;
   const Rows queries(a.q_span, b, a.q_total, a.q_rows), keys(a.k_span, b, a.k_total, a.k_rows);
-  const int q0 = q_tile * kTileQueries;
-  if (q0 >= queries.count) return;
-  const int mine = q0 + 32 * wave + r;                        // this lane's query
-  const bool there = mine < queries.count;
+  {
+    // nothing to do where all of the tile's queries are behind the sequence's end
+    const int row = a.share == 1 ? u.q_tile * kTileQueries : u.q_tile * kTileQueries % a.q_rows;
+    if (queries.count == 0 || (row >= queries.count && (a.share == 1 || row + kTileQueries <= a.q_rows))) return;
+  }
   const int k_count = uniform(keys.count);
   const int from = uniform(part * a.tiles_of_part), to = uniform(min(split ? from + a.tiles_of_part : INT32_MAX, (k_count + KEYS - 1) / KEYS));
 
-  const int kv_head = uniform(head / a.share);
   const T* K = uniform(static_cast<const T*>(a.K) + ((a.k_span ? 0 : b * a.k.seq) + keys.first * a.k.row + kv_head * a.k.head));
   const T* V = uniform(static_cast<const T*>(a.V) + ((a.k_span ? 0 : b * a.v.seq) + keys.first * a.v.row + kv_head * a.v.head));
 
@@ -305,21 +323,28 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
   // ---- queries, as right operands ----
   constexpr int STEPS = W / (2 * E);                          // 16 bytes of a row for each half of the wave
   u32x4 q[STEPS];
+  bool idle;                                                  // a wave without queries
   {
-    const T* Q = static_cast<const T*>(a.Q) + ((a.q_span ? 0 : b * a.q.seq) + (queries.first + q0) * a.q.row + head * a.q.head);
-    if (DIRECT) {                                             // all at once, zeros for rows and columns that are not there
-      const int rows = min(kTileQueries, queries.count - q0), bytes = (int)(a.q.row * sizeof(T));
-      const auto from_here = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(uniform(Q)), 0, uniform((rows - 1) * bytes + row_bytes), 0x00027000);
+    const Query mine(a, u, 32 * wave + r, queries.count);
+    idle = __builtin_amdgcn_ballot_w64(mine.there) == 0;
+    const T* Q = static_cast<const T*>(a.Q) + ((a.q_span ? 0 : b * a.q.seq) + (mine.there ? mine.at(a.q, queries.first) : queries.first * a.q.row));
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        const uint32_t at = there && (2 * s + h) * 16 < row_bytes ? (uint32_t)((32 * wave + r) * bytes + (2 * s + h) * 16) : 0x80000000u;
-        q[s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_here, at, 0, 0));
+    for (int s = 0; s < STEPS; ++s) {
+      const bool present = mine.there && (2 * s + h) * 16 < row_bytes;
+      if (DIRECT)
+        q[s] = *reinterpret_cast<const u32x4*>(Q + (present ? (2 * s + h) * E : 0));
+      else
+        q[s] = load_chunk(Q, 0, 0, 2 * s + h, mine.there);
+    }
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const bool present = mine.there && (2 * s + h) * 16 < row_bytes;
+      if (DIRECT) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[s][e] = present ? q[s][e] : 0u;
+      } else {
+        q[s] = chunk_of(q[s], 2 * s + h, mine.there);
       }
-    } else {
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) q[s] = load_chunk(Q, a.q.row, there ? 32 * wave + r : 0, 2 * s + h, true);
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) q[s] = chunk_of(q[s], 2 * s + h, true);
     }
   }
 
@@ -349,7 +374,7 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
 
   // The products of a step are dealt out over the softmax's other work, so that both units are busy: `between(n, all)` does the n-th of `all` shares of it behind the n-th
   // product.
-  constexpr int AHEAD = G::F32 && W == 256 ? 1 : 3;                     // operands are read from LDS so many products ahead, as many as there are registers for
+  constexpr int AHEAD = !G::F32 || W < 128 ? 3 : W == 128 ? 2 : 1;                    // operands are read from LDS so many products ahead, as many as there are registers for
   constexpr int KEY_PRODUCTS = STEPS * BLOCKS, VALUE_PRODUCTS = G::F32 ? 16 * BLOCKS : 2 * BLOCKS * (W / 32);
   u32x4 k[AHEAD + 1];
   bf16x8 v[AHEAD + 1];
@@ -501,7 +526,7 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
       __syncthreads();
   };
 
-  if (DIRECT && q0 + 32 * wave >= queries.count) {
+  if (DIRECT && idle) {
     // a wave without queries loads its share of the tiles
     if (from < to) begin();
     for (int tile = from; tile + 1 < to; ++tile) {
@@ -574,7 +599,10 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
     const float x = __shfl(sums[0], lane % 16), y = __shfl(sums[1], lane % 16);
     sum = lost | __shfl_xor(lost, 32) ? NAN : lane & 16 ? y : x;
   }
-  if (!there) return;
+  int own = 32 * wave + r;
+  asm volatile("" : "+v"(own));                                // made anew, not kept in registers all along
+  const Query mine(a, u, own, queries.count);
+  if (!mine.there) return;
   if (split) {
     const int64_t at = ((int64_t)(unit - a.whole) * a.parts + part) * kTileQueries + 32 * wave + r;
     if (h == 0) {
@@ -586,7 +614,7 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
     return;
   }
   const float share = sum == 0.f ? 0.f : 1.f / sum;
-  T* Out = static_cast<T*>(a.Out) + ((a.q_span ? 0 : b * a.o.seq) + (queries.first + mine) * a.o.row + head * a.o.head);
+  T* Out = static_cast<T*>(a.Out) + ((a.q_span ? 0 : b * a.o.seq) + mine.at(a.o, queries.first));
 #pragma unroll
   for (int d = 0; d < W / 32; ++d) {
 #pragma unroll
@@ -609,8 +637,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   const int id = uniform(blockIdx.x * 4 + threadIdx.x / kWave), n = id / kTileQueries, i = id % kTileQueries;
   const Unit u(a, a.whole + n);
   const Rows queries(a.q_span, u.b, a.q_total, a.q_rows);
-  const int row = u.q_tile * kTileQueries + i;
-  if (row >= queries.count) return;
+  const Query mine(a, u, i, queries.count);
+  if (!mine.there) return;
   const int64_t first = (int64_t)n * a.parts * kTileQueries + i;
   float top = -INFINITY, sum = 0.f;                            // of part `lane`
   if (lane < a.parts) {
@@ -641,7 +669,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
     }
   }
   const float share = total == 0.f ? 0.f : 1.f / total;
-  T* Out = static_cast<T*>(a.Out) + ((a.q_span ? 0 : u.b * a.o.seq) + (queries.first + row) * a.o.row + u.head * a.o.head);
+  T* Out = static_cast<T*>(a.Out) + ((a.q_span ? 0 : u.b * a.o.seq) + mine.at(a.o, queries.first));
 #pragma unroll
   for (int e = 0; e < EACH; ++e)
     if (64 * e + lane < a.head_dim) st_elem(Out, 64 * e + lane, o[e] * share);
@@ -693,7 +721,7 @@ int32_t launch_attention(const svdc_attention& p, const void* Q, const void* K, 
   const bool direct = p.head_dim % unit == 0 && sixteen(Q, p.q, q_span) && sixteen(K, p.k, k_span) && sixteen(V, p.v, k_span);
   const AttentionArgs a{Q, K, V, Out, reinterpret_cast<const int2*>(q_span), reinterpret_cast<const int2*>(k_span), key_mask,
                         static_cast<float*>(workspace), reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + sums_bytes(p, plan)),
-                        p.q_total, p.k_total, p.q, p.k, p.v, p.o, (int)p.batch, p.heads, p.heads / p.kv_heads, p.head_dim, (int)p.q_rows, (int)p.k_rows,
+                        p.q_total, p.k_total, p.q, p.k, p.v, p.o, p.kv_heads, p.heads / p.kv_heads, p.head_dim, (int)p.q_rows, (int)p.k_rows,
                         plan.q_tiles, plan.whole, plan.units, plan.parts, plan.tiles_of_part, p.scale * 1.4426950408889634f};
   p.dtype == SVDC_F32 ? attention_by_width<float>(a, direct, st) : attention_by_width<bf16_t>(a, direct, st);
   return launch_status();

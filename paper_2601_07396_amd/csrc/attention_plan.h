@@ -17,7 +17,7 @@ constexpr int attention_tile_keys(int width, bool f32) { return !f32 && width <=
 constexpr int kTileQueries = 128;      // that a workgroup has, 32 a wave
 constexpr int kLeastTiles = 2;         // of a part
 
-// Units of work are tiles of queries of a head: batch * heads * q_tiles.  The first `whole` of them are a workgroup's each, with all keys; each of the others is cut into `parts` parts of
+// Units of work are tiles of the queries of all heads that share a head of keys: batch * kv_heads * q_tiles.  The first `whole` of them are a workgroup's each, with all keys; each of the others is cut into `parts` parts of
 // tiles_of_part tiles of keys, a workgroup's each, which a second launch joins.  Without others parts is 1.
 struct AttentionPlan {
   int q_tiles, units, whole, parts, tiles_of_part;
@@ -28,8 +28,8 @@ constexpr int kMostParts = 64;         // a lane each when they are joined
 inline AttentionPlan attention_plan(const svdc_attention& p, int cus) {
   const int width = attention_width(p.head_dim), keys = attention_tile_keys(width, p.dtype == SVDC_F32);
   AttentionPlan plan{};
-  plan.q_tiles = (int)((p.q_rows + kTileQueries - 1) / kTileQueries);
-  plan.units = (int)(p.batch * p.heads * plan.q_tiles);
+  plan.q_tiles = (int)((p.heads / p.kv_heads * p.q_rows + kTileQueries - 1) / kTileQueries);
+  plan.units = (int)(p.batch * p.kv_heads * plan.q_tiles);
   plan.whole = plan.units;
   plan.parts = 1;
   const int64_t tiles = std::max<int64_t>(1, (p.k_rows + keys - 1) / keys);
@@ -41,8 +41,8 @@ inline AttentionPlan attention_plan(const svdc_attention& p, int cus) {
   plan.tiles_of_part = (int)tiles;
   const int rest = plan.units % cus;
   if (plan.units > 0 && plan.units < cus) {
-    // Fewer units than compute units: parts of all, until each of these has two workgroups.  64 x 119056, 24 heads: 21 parts 275 us (whole: 24 workgroups).  1 x 512, 24 heads: 4 parts
-    // 9.7 us, whole 10.5
+    // Fewer units than compute units: parts of all, until each of these has two workgroups.  64 x 119056, 24 heads: 21 parts 270 us.  1 x 512, 24 heads: 4 parts 8.7 us,
+    // whole 10.5
     cut(0, std::min<int64_t>(std::min<int64_t>(std::max(1, 2 * cus / plan.units), kMostParts), (tiles + kLeastTiles - 1) / kLeastTiles));
   } else if (rest) {
     // The last round has work for some of the compute units only: its units in parts, if that takes less than what the parts' sums cost on their way through memory.

@@ -70,7 +70,7 @@ int32_t check_attention(const svdc_attention* p, bool q_span, bool k_span) {
       p->heads % p->kv_heads != 0 || p->head_dim < 1 || p->head_dim > kMaxHeadDim)
     return SVDC_E_SHAPE;
   // units of work, each at most 64 workgroups
-  if (p->batch * p->heads * ((p->q_rows + 127) / 128) > (1 << 24)) return SVDC_E_SHAPE;
+  if (p->batch * p->heads * ((p->q_rows + 127) / 128) > (1 << 23)) return SVDC_E_SHAPE;
   if (q_span && (p->q_total < 0 || p->q_total > INT32_MAX)) return SVDC_E_SHAPE;
   if (k_span && (p->k_total < 0 || p->k_total > INT32_MAX)) return SVDC_E_SHAPE;
   if (!heads_ok(p->q, !q_span) || !heads_ok(p->o, !q_span) || !heads_ok(p->k, !k_span) || !heads_ok(p->v, !k_span)) return SVDC_E_SHAPE;

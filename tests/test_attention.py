@@ -73,6 +73,7 @@ SIZES = [  # batch, queries, keys, heads, heads of keys, head_dim
     (1, 1, 1, 1, 1, 128), (1, 1, 512, 24, 24, 128), (2, 33, 65, 3, 3, 128), (1, 128, 64, 2, 2, 128), (1, 129, 191, 2, 1, 128), (2, 257, 300, 4, 2, 64),
     (1, 40, 1000, 6, 2, 72), (3, 31, 97, 5, 5, 80), (1, 300, 200, 2, 2, 96), (1, 70, 130, 2, 2, 256), (1, 300, 90, 1, 1, 256), (2, 64, 64, 4, 4, 8),
     (1, 50, 77, 3, 1, 33), (1, 17, 40, 2, 2, 1), (1, 140, 333, 2, 2, 130), (1, 9, 5000, 2, 2, 128), (1, 3, 9000, 1, 1, 40), (2, 513, 700, 2, 2, 128),
+    (2, 7, 300, 41, 1, 72), (1, 1, 2000, 24, 3, 128), (1, 200, 260, 6, 2, 128), (2, 127, 90, 9, 3, 64), (1, 5, 130, 130, 1, 33),
 ]
 
 
@@ -169,7 +170,7 @@ def test_numbers_at_the_ends(m, dtype):
 @pytest.mark.parametrize("cross", [False, True])
 def test_spans(cross, masked, dtype):
     """Packed and padded sequences, empty ones, a single row, spans that leave the tensors: rows of no span stay as they were."""
-    h, hk, d, total, k_total = 4, 2, 64, 700, 900 if cross else 700
+    h, hk, d, total, k_total = 6, 2, 64, 700, 900 if cross else 700
     g = torch.Generator().manual_seed(11)
     q, k, v = heads(g, 1, total, h, d, dtype)[0], heads(g, 1, k_total, hk, d, dtype)[0], heads(g, 1, k_total, hk, d, dtype)[0]
     q_of = [(0, 129), (129, 1), (130, 0), (140, 200), (690, 300), (400, 77), (-20, 0), (900, 5), (350, 50), (2 ** 31 - 1, 2 ** 31 - 1), (-3, -4)]
@@ -326,7 +327,7 @@ def status(p, Q=POINTER, K=2 * POINTER, V=3 * POINTER, q_span=0, k_span=0, mask=
     (dict(dtype=2), -3), (dict(dtype=-1), -3), (dict(scale=0.0), -5), (dict(scale=-1.0), -5), (dict(scale=math.inf), -5), (dict(scale=math.nan), -5),
     (dict(reserved=1), -5), (dict(batch=-1), -2), (dict(batch=65536), -2), (dict(q_rows=-1), -2), (dict(k_rows=2 ** 31), -2), (dict(batch=3, q_rows=2 ** 30), -2),
     (dict(heads=0), -2), (dict(heads=3), -2), (dict(kv_heads=0), -2), (dict(heads=2 ** 16 + 2), -2), (dict(head_dim=0), -2), (dict(head_dim=257), -2),
-    (dict(heads=2 ** 16, q_rows=2 ** 20), -2), (dict(q=svdc.Heads(-1, 0, 0)), -2), (dict(k=svdc.Heads(0, 2 ** 22 + 1, 0)), -2),
+    (dict(heads=2 ** 16, q_rows=2 ** 20), -2), (dict(batch=1, heads=2 ** 14, kv_heads=1, q_rows=2 ** 16 + 1), -2), (dict(q=svdc.Heads(-1, 0, 0)), -2), (dict(k=svdc.Heads(0, 2 ** 22 + 1, 0)), -2),
     (dict(v=svdc.Heads(0, 0, 2 ** 40 + 1)), -2), (dict(o=svdc.Heads(2 ** 40 + 1, 0, 0)), -2), (dict(k=svdc.Heads(0, -5, 0)), -2)])
 def test_refused_descriptors(fields, code):
     p = descriptor(**fields)

@@ -13,13 +13,13 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PROGRAM = r"""
 #include <cstdio>
 #include "attention_plan.h"
-// batch q_rows k_rows heads head_dim dtype cus -> q_tiles units whole parts tiles_of_part, keys of a tile
+// batch q_rows k_rows heads share head_dim dtype cus -> q_tiles units whole parts tiles_of_part, keys of a tile
 int main() {
   long long batch, q, k;
-  int heads, d, dtype, cus;
-  while (std::scanf("%lld %lld %lld %d %d %d %d", &batch, &q, &k, &heads, &d, &dtype, &cus) == 7) {
+  int heads, share, d, dtype, cus;
+  while (std::scanf("%lld %lld %lld %d %d %d %d %d", &batch, &q, &k, &heads, &share, &d, &dtype, &cus) == 8) {
     svdc_attention p{};
-    p.batch = batch, p.q_rows = q, p.k_rows = k, p.heads = heads, p.kv_heads = heads, p.head_dim = d, p.dtype = dtype;
+    p.batch = batch, p.q_rows = q, p.k_rows = k, p.heads = heads * share, p.kv_heads = heads, p.head_dim = d, p.dtype = dtype;
     const svdc::AttentionPlan plan = svdc::attention_plan(p, cus);
     std::printf("%d %d %d %d %d %d\n", plan.q_tiles, plan.units, plan.whole, plan.parts, plan.tiles_of_part, svdc::attention_tile_keys(svdc::attention_width(d), dtype == 0));
   }
@@ -45,14 +45,15 @@ def plans(tmp_path_factory):
 def test_every_key_once(plans):
     """Units cover the queries, parts the keys, none of them is empty, and a lane each is enough to join them."""
     rng = random.Random(1)
-    cases = [(1, 1, 1, 1, 1, 0, 256), (1, 1, 0, 1, 1, 1, 256), (1, 2 ** 30, 2 ** 30, 2, 256, 0, 256), (65535, 1, 2 ** 15, 256, 64, 1, 256), (1, 1, 2 ** 30, 1, 8, 1, 304)]
+    cases = [(1, 1, 1, 1, 1, 1, 0, 256), (1, 1, 0, 1, 1, 1, 1, 256), (1, 2 ** 30, 2 ** 30, 1, 1, 256, 0, 256), (1, 2 ** 14, 2 ** 30, 1, 2 ** 16, 256, 0, 256),
+             (65535, 1, 2 ** 15, 128, 1, 64, 1, 256), (1, 1, 2 ** 30, 1, 1, 8, 1, 304)]
     for _ in range(4000):
         batch, heads = rng.choice([1, 1, 2, 5, 31]), rng.choice([1, 3, 8, 24, 40])
-        cases.append((batch, int(2 ** rng.uniform(0, 17)), int(2 ** rng.uniform(0, 18)), heads, rng.choice([8, 64, 72, 128, 200, 256]), rng.randint(0, 1), rng.choice([1, 32, 256, 304])))
+        cases.append((batch, int(2 ** rng.uniform(0, 17)), int(2 ** rng.uniform(0, 18)), heads, rng.choice([1, 1, 3, 8]), rng.choice([8, 64, 72, 128, 200, 256]), rng.randint(0, 1), rng.choice([1, 32, 256, 304])))
     for case, (q_tiles, units, whole, parts, each, keys) in zip(cases, plans(cases)):
-        batch, q, k, heads, _, _, cus = case
+        batch, q, k, heads, share, _, _, cus = case
         tiles = max(1, -(-k // keys))
-        assert q_tiles == -(-q // 128) and units == batch * heads * q_tiles
+        assert q_tiles == -(-q * share // 128) and units == batch * heads * q_tiles
         assert 0 <= whole <= units and 1 <= parts <= 64
         assert parts * each >= tiles and (parts - 1) * each < tiles, case
         assert (whole == units) == (parts == 1)
@@ -61,10 +62,10 @@ def test_every_key_once(plans):
 
 
 def test_few_rows_fill_the_card(plans):
-    for case in ((1, 64, 119056, 24, 128, 1, 256), (1, 1, 20000, 8, 128, 1, 256), (2, 100, 30000, 5, 64, 0, 256)):
+    for case in ((1, 64, 119056, 24, 1, 128, 1, 256), (1, 1, 20000, 8, 1, 128, 1, 256), (1, 1, 20000, 8, 4, 128, 1, 256), (2, 100, 30000, 5, 1, 64, 0, 256)):
         (_, units, whole, parts, _, _), = plans([case])
         assert whole == 0 and units * parts > 256
-    for case in ((1, 1, 60, 24, 128, 1, 256), (1, 32768, 4096, 2, 128, 1, 256)):      # one tile; two rounds exactly
+    for case in ((1, 1, 60, 24, 1, 128, 1, 256), (1, 32768, 4096, 2, 1, 128, 1, 256), (1, 4096, 4096, 2, 8, 128, 1, 256)):      # one tile; two rounds exactly
         (_, units, whole, _, _, _), = plans([case])
         assert whole == units
 
