@@ -508,7 +508,7 @@ size_t svdcache_attention_workspace_bytes(const svdc_attention* p);
  *   workspace      device scratch of svdcache_attention_workspace_bytes() bytes, 256-byte aligned, NULL where that is 0.  It belongs to the
  *                  call until it has completed on the stream: calls in flight on different streams need one each.
  * Pointers are aligned to their elements; rows and heads at multiples of 16 bytes of one another (pointers, strides and head_dim) are read faster.
- * Products and sums, the softmax's maximum and sum are float32.  For bfloat16 the probabilities enter the second product rounded to
+ * Products and sums, the softmax's maximum and sum are float32.  Products that float32 holds give finite results, however large scale times them is.  For bfloat16 the probabilities enter the second product rounded to
  * bfloat16, which is as much off as rounding the result is; float32 uses float32 products throughout.  The exponential is the hardware's power of two (a step of the last place).  Results do not depend on anything but the
  * arguments and the number of compute units (no atomics). */
 int32_t svdcache_attention(const svdc_attention* p, const void* Q, const void* K, const void* V, const int32_t* q_span, const int32_t* k_span,

@@ -35,7 +35,7 @@ struct AttentionArgs {
   void* Out;
   const int2 *q_span, *k_span;
   const uint8_t* mask;
-  float *sums, *stats;               // of parts: [unit][part][query][width] and [..][2]: what was subtracted from the exponents, and their powers' sum
+  float *sums, *stats, *large;       // of parts: [unit][part][query][width]; [..][2]: what was subtracted from the exponents, and their powers' sum; [..]: where that is large, its product
   int64_t q_total, k_total;
   svdc_heads q, k, v, o;
   int kv_heads, share, head_dim, q_rows, k_rows, q_tiles, whole, units, parts, tiles_of_part;
@@ -125,6 +125,7 @@ struct Tile {
 };
 
 constexpr int WAVES = kTileQueries / 32;                       // of a workgroup
+constexpr float SLACK = 6.f, LARGE = 65536.f;                  // of what is subtracted from the exponents: how far above the maximum it begins, and from where on it is coarse
 
 template <int BYTES>
 struct Lds {
@@ -355,6 +356,7 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
   // Their sums.  bfloat16: made by a 16 x 16 product, for which lanes 16 g .. 16 g + 15 are columns 0 .. 15 with eight numbers of the summed axis each.  Ones in row 0 for even g,
   // which hold queries 0 .. 15, and in row 1 for odd g, which hold queries 16 .. 31: lane n's sums[0] is query n's, sums[1] query 16 + n's.
   float shift = -INFINITY, sum = 0.f;
+  uint64_t coarse = 0;                                        // lanes whose shift is large, and kept as the product that it lies SLACK above
   f32x4 sums = {};
   int lost = 0;
   const uint32_t one_here = lane % 16 == lane / 16 % 2 ? 0x3f803f80u : 0u;
@@ -488,19 +490,39 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
   };
   // What is subtracted from the exponents may be any number not far from the maximum: it stays until a probability passes 2, then follows to SLACK above the maximum, and the
   // tile's probabilities are made again.  -infinity until there is a key: then everything passes.
-  constexpr float SLACK = 6.f;
-  const auto follow = [&](const f32x16 (&s)[BLOCKS]) INLINE {
-    if (__builtin_amdgcn_ballot_w64((over & (G::F32 ? 0x40000000u : 0x40004000u)) != 0) == 0) return;
+  // Below 2^16 the roundings of a shift move an exponent by 2^-7 at most.  From there on (coarse) they would in the end pass SLACK, or the shift float32: the exponents are made of the
+  // products' distances from the largest one, which are exact for equal products, and every tile's probabilities are made again.  (coarse is a mask in scalar registers, and the shift holds
+  // that product, because the masked float32 kernel of 128 columns has no vector register left.)
+  const auto follow = [&](f32x16 (&s)[BLOCKS]) INLINE {
+    constexpr uint32_t TOP = G::F32 ? 0x40000000u : 0x40004000u;
+    if ((__builtin_amdgcn_ballot_w64((over & TOP) != 0) | coarse) == 0) return;
     float high = -INFINITY;
 #pragma unroll
     for (int t = 0; t < BLOCKS; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) high = fmaxf(high, s[t][i]);
-    high = max_of_halves(high) * a.scale;
-    const bool up = !(high - shift < 0.5f);                    // 2 and what rounds to it is well above: behind this, only what is no number still passes
+    const float product = max_of_halves(high);
+    high = product * a.scale;
     const float before = shift;
+    // 2 and what rounds to it is well above: behind this, only what is no number still passes
+    bool up = !(high - shift < 0.5f), large = up && product != -INFINITY && !(fabsf(high + SLACK) < LARGE);
     if (up) shift = high + SLACK;
-    const float less = !up ? 1.f : before == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(before - shift);
+    float less = !up ? 1.f : before == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(before - shift), by = shift == -INFINITY ? 0.f : shift;
+    float off = 0.f;
+    if (__builtin_expect((coarse | __builtin_amdgcn_ballot_w64(large)) != 0, 0)) {
+      const bool was_large = coarse >> lane & 1;
+      if (was_large) {
+        up = !((product - before) * a.scale < SLACK + 0.5f);
+        large = !up || !(fabsf(high + SLACK) < LARGE);
+        shift = !up ? before : large ? product : high + SLACK;
+        less = !up ? 1.f : __builtin_amdgcn_exp2f(large ? (before - product) * a.scale : before * a.scale + SLACK - shift);
+      } else if (large) {
+        shift = product;
+      }
+      coarse = __builtin_amdgcn_ballot_w64(large);
+      by = large ? SLACK : shift == -INFINITY ? 0.f : shift;
+      off = large ? shift : 0.f;
+    }
     sum *= less;
     sums[0] *= less;
     sums[1] *= __shfl(less, lane % 16 + 16);
@@ -508,10 +530,13 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
     for (int d = 0; d < W / 32; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] *= less;
-    const float by = shift == -INFINITY ? 0.f : shift;
+#pragma unroll
+    for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] -= off;
 #pragma unroll
     for (int n = 0; n < 8; ++n) probabilities(s, by, n, 8);
-    if (!G::F32 && (over & 0x40004000u)) {                     // no number: not into a column that another query's sum comes from, but into the result
+    if (!G::F32 && (over & TOP)) {                             // no number: not into a column that another query's sum comes from, but into the result
       lost = 1;
 #pragma unroll
       for (int i = 0; i < 2 * BLOCKS; ++i) p[i] = u32x4{};
@@ -606,8 +631,10 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
   if (split) {
     const int64_t at = ((int64_t)(unit - a.whole) * a.parts + part) * kTileQueries + 32 * wave + r;
     if (h == 0) {
-      a.stats[2 * at] = sum == 0.f ? -INFINITY : fmaxf(shift, -3.4e38f);   // a sum that is no number counts
+      const float top = fmaxf(coarse >> lane & 1 ? __builtin_fmaf(shift, a.scale, SLACK) : shift, -3.4e38f);
+      a.stats[2 * at] = sum == 0.f ? -INFINITY : top;          // a sum that is no number counts
       a.stats[2 * at + 1] = sum;
+      if (!(fabsf(top) < LARGE)) a.large[at] = shift;
     }
 #pragma unroll
     for (int d = 0; d < W / 32; ++d) store_columns<float>(a.sums + at * W, 32 * d, W, o[d], h);
@@ -630,6 +657,12 @@ __global__ __launch_bounds__(64 * WAVES, W <= 128 && DIRECT ? 2 : 1) void attent
 #endif
 }
 
+__device__ __forceinline__ float max_of_wave(float v) {
+#pragma unroll
+  for (int e = 32; e > 0; e >>= 1) v = fmaxf(v, __shfl_xor(v, e));
+  return v;
+}
+
 // Joins the parts of the keys, a wave for each query of the units that were split: lane l's columns are l, l + 64, ...
 template <typename T, int W>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
@@ -640,26 +673,33 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   const Query mine(a, u, i, queries.count);
   if (!mine.there) return;
   const int64_t first = (int64_t)n * a.parts * kTileQueries + i;
-  float top = -INFINITY, sum = 0.f;                            // of part `lane`
-  if (lane < a.parts) {
-    const float2 s = reinterpret_cast<const float2*>(a.stats)[first + lane * kTileQueries];
-    top = s.x, sum = s.y;
-  }
-  float high = top;
-#pragma unroll
-  for (int e = 32; e > 0; e >>= 1) high = fmaxf(high, __shfl_xor(high, e));
-  const float weight = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - high);
-  const float total = wave_sum(top == -INFINITY ? 0.f : weight * sum);
   constexpr int EACH = (W + 63) / 64, AT_ONCE = 8 / EACH;       // loads in flight
-  float o[EACH] = {};
   const float* from = a.sums + first * W + lane;
-  for (int p0 = 0; p0 < a.parts; p0 += AT_ONCE) {
-    float x[AT_ONCE][EACH];
+  float x[AT_ONCE][EACH];
+  const auto load = [&](int p0) INLINE {
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
       for (int e = 0; e < EACH; ++e)
         if (64 * e + lane < W) x[i][e] = from[(int64_t)min(p0 + i, a.parts - 1) * kTileQueries * W + 64 * e];
+  };
+  float top = -INFINITY, sum = 0.f;                            // of part `lane`
+  if (lane < a.parts) {
+    const float2 s = reinterpret_cast<const float2*>(a.stats)[first + lane * kTileQueries];
+    top = s.x, sum = s.y;
+  }
+  load(0);
+  float distance = top - max_of_wave(top);
+  const bool large = top != -INFINITY && !(fabsf(top) < LARGE);
+  if (__builtin_amdgcn_ballot_w64(large)) {                    // their own differences are too coarse, or none
+    const float product = large ? a.large[first + lane * kTileQueries] : (top - SLACK) / a.scale;
+    distance = (product - max_of_wave(product)) * a.scale;
+  }
+  const float weight = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(distance);
+  const float total = wave_sum(top == -INFINITY ? 0.f : weight * sum);
+  float o[EACH] = {};
+  for (int p0 = 0; p0 < a.parts; p0 += AT_ONCE) {
+    if (p0) load(p0);
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
       const float w = __shfl(weight, (p0 + i) % kWave);        // 0 behind the last part and for one without keys, whose sums were not written
@@ -698,17 +738,14 @@ void attention_by_width(const AttentionArgs& a, bool direct, hipStream_t st) {
   }
 }
 
-// bytes of the parts' sums, a multiple of 256, and of their statistics
-size_t sums_bytes(const svdc_attention& p, const AttentionPlan& plan) {
-  return (size_t)(plan.units - plan.whole) * plan.parts * kTileQueries * attention_width(p.head_dim) * sizeof(float);
-}
-size_t stats_bytes(const AttentionPlan& plan) { return (size_t)(plan.units - plan.whole) * plan.parts * kTileQueries * 2 * sizeof(float); }
+// Queries of all parts: a multiple of 128.  Their sums, their statistics and their large shifts' products lie one behind the other.
+size_t part_queries(const AttentionPlan& plan) { return (size_t)(plan.units - plan.whole) * plan.parts * kTileQueries; }
 
 }  // namespace
 
 size_t attention_workspace_bytes(const svdc_attention& p) {
   const AttentionPlan plan = attention_plan(p, num_compute_units());
-  return sums_bytes(p, plan) + stats_bytes(plan);
+  return part_queries(plan) * (attention_width(p.head_dim) + 3) * sizeof(float);
 }
 
 int32_t launch_attention(const svdc_attention& p, const void* Q, const void* K, const void* V, const int32_t* q_span, const int32_t* k_span,
@@ -719,8 +756,9 @@ int32_t launch_attention(const svdc_attention& p, const void* Q, const void* K, 
     return reinterpret_cast<uintptr_t>(x) % 16 == 0 && s.row % unit == 0 && s.head % unit == 0 && (spans || s.seq % unit == 0);
   };
   const bool direct = p.head_dim % unit == 0 && sixteen(Q, p.q, q_span) && sixteen(K, p.k, k_span) && sixteen(V, p.v, k_span);
+  float* const stats = static_cast<float*>(workspace) + part_queries(plan) * attention_width(p.head_dim);
   const AttentionArgs a{Q, K, V, Out, reinterpret_cast<const int2*>(q_span), reinterpret_cast<const int2*>(k_span), key_mask,
-                        static_cast<float*>(workspace), reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + sums_bytes(p, plan)),
+                        static_cast<float*>(workspace), stats, stats + 2 * part_queries(plan),
                         p.q_total, p.k_total, p.q, p.k, p.v, p.o, p.kv_heads, p.heads / p.kv_heads, p.head_dim, (int)p.q_rows, (int)p.k_rows,
                         plan.q_tiles, plan.whole, plan.units, plan.parts, plan.tiles_of_part, p.scale * 1.4426950408889634f};
   p.dtype == SVDC_F32 ? attention_by_width<float>(a, direct, st) : attention_by_width<bf16_t>(a, direct, st);

@@ -380,3 +380,87 @@ def test_binding_refuses():
         svdc.svdcache_attention(p, q[0], k[0], k[0], q[0], span[:2], span)
     with pytest.raises(ValueError, match="span"):
         svdc.svdcache_attention(p, q[0], k[0], k[0], q[0], span.long(), span)
+
+
+# ---- logits whose float32 steps pass the probabilities' range ---------------------------------------------------------
+#
+# Whole numbers times a power of two: float32 products and sums of them are exact, equal logits are equal bits, and logits that differ lie at least 2^16 apart, a probability of zero.  So
+# e of the tolerances above is 2^-22 whatever the logits are, and ref's softmax of the exact products says how many keys share the probability.
+
+def check_exact_products(got, q, k, v, scale, dtype):
+    o, A, _ = ref(q, k, v, scale)
+    u, rounded = (2.0 ** -8, 2.0 ** -8) if dtype == BF16 else (2.0 ** -24, 0.0)
+    tol = 1.01 * (u * o.abs() + (2 * 2.0 ** -22 + 2 * k.shape[0] * 2.0 ** -24 + 2.0 ** -20 + rounded) * A)
+    assert torch.isfinite(got).all()
+    assert ((got.detach().cpu().double() - o).abs() <= tol).all()
+
+
+def whole_numbers(n, m, d, dtype, seed=20):
+    """Queries, and keys of which many are alike."""
+    g = torch.Generator().manual_seed(seed)
+    q, few = torch.randint(-3, 4, (1, n, 2, d), generator=g), torch.randint(-3, 4, (7, 2, d), generator=g)
+    k = few[torch.randint(0, 7, (m,), generator=g)][None]
+    return q.to(dtype).cuda(), k.to(dtype).cuda(), heads(g, 1, m, 2, d, dtype)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("steps,scale", [((8, 8), 2.0 ** 0), ((13, 14), 2.0 ** -3), ((20, 14), 2.0 ** -3), ((20, 20), 2.0 ** 0), ((60, 50), 2.0 ** 20), ((0, 0), 2.0 ** 126), ((60, 57), 2.0 ** -3)])
+@pytest.mark.parametrize("n,m,d", [(150, 300, 64), (40, 1000, 128), (3, 3000, 128), (33, 260, 74), (70, 200, 256), (3, 2500, 200)])
+def test_large_logits(n, m, d, steps, scale, dtype):
+    """Logits of 2^16 and far more, keys with the same one in many tiles and parts; larger and larger ones; none but negative ones."""
+    q, k, v = whole_numbers(n, m, d, dtype)
+    q, k = q * 2.0 ** steps[0], k * 2.0 ** steps[1]
+    out = like(q)
+    call(q, k, v, out, scale=scale)
+    check_exact_products(out[0], q[0], k[0], v[0], scale, dtype)
+    if n == 3:                                                  # 256 units, a whole one each
+        many = [t.expand(128, *t.shape[1:]) for t in (q, k, v)]
+        all_out = torch.full(many[0].shape, float("nan"), device="cuda", dtype=dtype)
+        assert svdc.svdcache_attention_workspace_bytes(call(*many, all_out, scale=scale)) == 0
+        check_exact_products(all_out[77], q[0], k[0], v[0], scale, dtype)
+    call(-q.abs(), k.abs() + 2.0 ** steps[1], v, out, scale=scale)
+    check_exact_products(out[0], -q[0].abs(), k[0].abs() + 2.0 ** steps[1], v[0], scale, dtype)
+    rising = k * (torch.arange(m, device="cuda") // 50 % 8).to(dtype)[None, :, None, None]
+    if steps != (60, 57):                                       # eight times as much passes float32
+        call(q, rising, v, out, scale=scale)
+        check_exact_products(out[0], q[0], rising[0], v[0], scale, dtype)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("size", [1e8, 1e9, 1e11, 1e20])
+@pytest.mark.parametrize("n,m,d", [(200, 300, 128), (3, 3000, 64)])
+def test_large_random_logits(n, m, d, size, dtype):
+    """Numbers that are not exact: the best key takes all wherever the others are further below it than the products' rounding."""
+    g = torch.Generator().manual_seed(21)
+    q, k, v = (heads(g, 1, rows, 2, d, dtype) for rows in (n, m, m))
+    q = q * size ** 0.5
+    k = k * size ** 0.5
+    out = like(q)
+    call(q, k, v, out)
+    check(out[0], q[0], k[0], v[0], d ** -0.5, dtype)
+    for head in range(2):
+        s = d ** -0.5 * q[0, :, head].cpu().double() @ k[0, :, head].cpu().double().T
+        B = d ** -0.5 * float((q[0, :, head].cpu().double().abs() @ k[0, :, head].cpu().double().abs().T).max())
+        two = s.topk(2, dim=1)
+        alone = (two.values[:, 0] - two.values[:, 1] > 2 * (d + 8) * 2.0 ** -24 * B + 40).nonzero()[:, 0]
+        assert len(alone) >= 1
+        want = v[0, two.indices[alone, 0].cuda(), head].double()
+        tol = 1.01 * (2.0 ** -8 * 2 + 2.0 ** -20 if dtype == BF16 else 2.0 ** -20 + 2.0 ** -22) * want.abs() + 2.0 ** -40 * v.abs().max().double()
+        assert ((out[0, alone.cuda(), head].double() - want).abs() <= tol).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,m", [(64, 500), (9, 3000)])
+def test_large_logits_beside_ordinary_ones(n, m, dtype):
+    """One query of a tile with large logits, with infinite ones, or without a number: the others are as near as ever."""
+    g = torch.Generator().manual_seed(22)
+    q, k, v = (heads(g, 1, rows, 2, 128, dtype) for rows in (n, m, m))
+    out, others = like(q), [i for i in range(n) if i != 5]
+    for bad in (1e9, 1e30, float("inf"), float("nan")):
+        q[:, 5] = bad
+        call(q, k, v, out)
+        check(out[0, others], q[0, others], k[0], v[0], 128 ** -0.5, dtype)
+        assert torch.isfinite(out[0, 5]).all() if math.isfinite(bad) else out[0, 5].isnan().all()
