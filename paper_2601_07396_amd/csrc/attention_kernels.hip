@@ -702,10 +702,10 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
     if (p0) load(p0);
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
-      const float w = __shfl(weight, (p0 + i) % kWave);        // 0 behind the last part and for one without keys, whose sums were not written
+      const float w = __shfl(weight, (p0 + i) % kWave);        // 0 for a part without keys, whose sums are zeros, and where float32 ends: times a NaN still NaN
 #pragma unroll
       for (int e = 0; e < EACH; ++e)
-        if (64 * e + lane < W && w != 0.f && p0 + i < a.parts) o[e] = __builtin_fmaf(w, x[i][e], o[e]);
+        if (64 * e + lane < W && p0 + i < a.parts) o[e] = __builtin_fmaf(w, x[i][e], o[e]);
     }
   }
   const float share = total == 0.f ? 0.f : 1.f / total;

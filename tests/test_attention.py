@@ -464,3 +464,30 @@ def test_large_logits_beside_ordinary_ones(n, m, dtype):
         call(q, k, v, out)
         check(out[0, others], q[0, others], k[0], v[0], 128 ** -0.5, dtype)
         assert torch.isfinite(out[0, 5]).all() if math.isfinite(bad) else out[0, 5].isnan().all()
+
+
+# ---- what lies in the tensors reaches the result, whole and in parts ---------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 74, 128, 200])
+def test_no_number_behind_a_small_probability(d, dtype):
+    """A NaN or an infinity among the values of a key whose probability is zero in float32 gives no number, whether the keys are cut into parts or not; other columns do not change."""
+    m, n = 3000, 3
+    g = torch.Generator().manual_seed(23)
+    q = torch.ones(1, n, 1, d, device="cuda", dtype=dtype)
+    k = torch.full((1, m, 1, d), -16.0, device="cuda", dtype=dtype)
+    k[:, 10] = 16.0
+    v = heads(g, 1, m, 1, d, dtype)
+    for at in (m - 1, m // 2):
+        bad = v.clone()
+        bad[0, at, 0, 3], bad[0, at, 0, 5] = float("nan"), float("inf")
+        for batch in (1, 256):                                   # a few parts each; 256 units, a whole one each
+            qq, kk, vv, clean = (t.expand(batch, *t.shape[1:]) for t in (q, k, bad, v))
+            out, want = torch.zeros(batch, n, 1, d, device="cuda", dtype=dtype), torch.zeros(batch, n, 1, d, device="cuda", dtype=dtype)
+            p = call(qq, kk, vv, out, scale=1.0)
+            assert (svdc.svdcache_attention_workspace_bytes(p) > 0) == (batch == 1)
+            call(qq, kk, clean, want, scale=1.0)
+            assert out[..., 3].isnan().all() and out[..., 5].isnan().all()
+            keep = [c for c in range(d) if c not in (3, 5)]
+            assert torch.equal(out[..., keep], want[..., keep]) and torch.isfinite(want).all()
