@@ -478,8 +478,11 @@ int32_t svdcache_norm_rotate(const svdc_norm_rotate* p, const void* Q, const voi
 }
 
 size_t svdcache_attention_workspace_bytes(const svdc_attention* p) {
-  // the strides of a sequence do not change it, and need not be there where spans are given
-  return check_attention(p, false, false) == SVDC_OK || check_attention(p, true, true) == SVDC_OK ? attention_workspace_bytes(*p) : 0;
+  // valid for a call with some of the spans: what that call does not read may hold anything
+  for (const bool q_span : {false, true})
+    for (const bool k_span : {false, true})
+      if (check_attention(p, q_span, k_span) == SVDC_OK) return attention_workspace_bytes(*p);
+  return 0;
 }
 
 int32_t svdcache_attention(const svdc_attention* p, const void* Q, const void* K, const void* V, const int32_t* q_span, const int32_t* k_span,

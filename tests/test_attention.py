@@ -491,3 +491,19 @@ def test_no_number_behind_a_small_probability(d, dtype):
             assert out[..., 3].isnan().all() and out[..., 5].isnan().all()
             keep = [c for c in range(d) if c not in (3, 5)]
             assert torch.equal(out[..., keep], want[..., keep]) and torch.isfinite(want).all()
+
+
+# ---- sizes of the workspace ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fields,spans", [
+    (dict(q=svdc.Heads(-1, 128, 64), o=svdc.Heads(2 ** 41, 128, 64), k_total=-1), dict(q_span=POINTER)),
+    (dict(k=svdc.Heads(-1, 128, 64), v=svdc.Heads(2 ** 41, 128, 64), q_total=2 ** 31), dict(k_span=POINTER)),
+    (dict(q=svdc.Heads(-1, 128, 64), v=svdc.Heads(-1, 128, 64)), dict(q_span=POINTER, k_span=POINTER)),
+    (dict(q_total=-1, k_total=2 ** 40), dict())])
+def test_workspace_size_reads_what_the_call_reads(fields, spans):
+    """Strides of a sequence where spans are given, and totals where none are, may hold anything."""
+    sizes = dict(batch=1, q_rows=1, k_rows=10000)
+    need = svdc.svdcache_attention_workspace_bytes(descriptor(**sizes))
+    p = descriptor(**sizes, **fields)
+    assert need > 0 and svdc.svdcache_attention_workspace_bytes(p) == need
+    assert status(p, ws=0, **spans) == -1 and status(p, bytes=need - 1, **spans) == -6
