@@ -444,8 +444,8 @@ typedef struct {
 } svdc_rotary;
 
 /* table[row][j] = (cos, sin) of pos[row][a] * theta[a]^(-2 i / dims[a]) with pair j the i-th of axis a.  Angles are made and reduced in 64 bits:
- * positions as far as 2^31 lose nothing (an angle is off by at most 2^-51 of itself, cosine and sine by less than 2^-22 more).  A position that
- * is not finite gives NaN.
+ * an angle is off by at most 2^-50 of itself whatever theta is, cosine and sine by less than 2^-22 more (with theta >= 1 and positions
+ * up to 2^28 by less than 2^-21 in all).  A position that is not finite gives NaN.
  *   pos    in   [rows, axes] float32 or int32
  *   table  out  [rows, pairs, 2] float32, dense, 8-byte aligned, with pairs = sum of dims / 2 */
 int32_t svdcache_rotary_table(const svdc_rotary* p, const void* pos, float* table, void* stream);

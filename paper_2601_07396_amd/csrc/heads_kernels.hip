@@ -6,6 +6,7 @@
 //     odd heads: 3 x 1001 rows, 16 + 8 heads of 72, 27 pairs of halves, float32 (42 MB) 12.7 us; one row 4.1 us, a launch
 // The angles are bound by their arithmetic in 64 bits: 119056 x 64 pairs (62 MB) 16 us, 3.9 TB/s; 4608 x 64 4.1 us.
 #include <algorithm>
+#include <cmath>
 
 #include "eight_bit.h"
 #include "svdc_internal.h"
@@ -24,11 +25,11 @@ struct RotaryArgs {
   int64_t rows, ld;
   int axes, pairs;
   int first[SVDC_MAX_AXES + 1];       // pair at which an axis begins
-  double theta[SVDC_MAX_AXES];
+  double theta[SVDC_MAX_AXES], log_theta[SVDC_MAX_AXES];      // by the number of the axis' pairs
 };
 
 // cos and sin of 2 pi t.  t is reduced to an eighth of a turn around the next quarter in 64 bits, where nothing is lost; what is left, 2^-28 of a turn off as a
-// float32, goes into the first terms of the two Taylor series: at pi / 4 the next ones are 2^-29 (sine) and 2^-31 (cosine).
+// float32, goes into the first terms of the two Taylor series: at pi / 4 the next ones are 2^-29 (sine) and 2^-33 (cosine).
 __device__ __forceinline__ float2 turn(double t) {
   const double whole = t - rint(t), quarter = rint(4.0 * whole);
   const float x = (float)__builtin_fma(quarter, -0.25, whole) * 6.2831853f, y = x * x;
@@ -50,7 +51,12 @@ __global__ __launch_bounds__(256) void rotary_table_kernel(RotaryArgs a) {
     for (int k = 1; k < SVDC_MAX_AXES; ++k)
       if (k < a.axes && j >= a.first[k]) axis = k;
     const int i = j - a.first[axis], n = a.first[axis + 1] - a.first[axis];
-    turns[j] = pow(a.theta[axis], -(double)i / n) * 0.15915494309189533577;   // 1 / (2 pi)
+    // What rounding the exponent left out, (-i - e n) / n, counts ln(theta) times: theta^(e + r) = theta^e (1 + r ln(theta)).
+    const double e = -(double)i / n;
+    float left = (float)(__builtin_fma(-e, n, -i) * a.log_theta[axis]);
+    asm volatile("" : "+v"(left));                            // one register across the power, where all are in use
+    const double power = pow(a.theta[axis], e);
+    turns[j] = __builtin_fma(power, left, power) * 0.15915494309189533577;   // 1 / (2 pi)
     axis_of[j] = axis;
   }
   __syncthreads();
@@ -336,12 +342,13 @@ void norm_rotate(const HeadsArgs& a, int layout, hipStream_t st) {
 }  // namespace
 
 int32_t launch_rotary_table(const svdc_rotary& p, const void* pos, float* table, hipStream_t st) {
-  RotaryArgs a{pos, table, p.rows, p.ld, p.axes, 0, {}, {}};
+  RotaryArgs a{pos, table, p.rows, p.ld, p.axes, 0, {}, {}, {}};
   for (int k = 0; k < p.axes; ++k) {
     a.first[k] = a.pairs;
     a.pairs += p.dims[k] / 2;
     a.first[k + 1] = a.pairs;
     a.theta[k] = p.theta[k];
+    a.log_theta[k] = std::log(p.theta[k]) / (p.dims[k] / 2);
   }
   const int64_t turns = (p.rows + 256 / a.pairs - 1) / (256 / a.pairs);
   const unsigned grid = (unsigned)std::min<int64_t>(turns, 8 * num_compute_units());

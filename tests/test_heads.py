@@ -8,6 +8,7 @@ Tolerances, derived:
 """
 import ctypes as C
 import math
+from decimal import Decimal, localcontext
 
 import numpy as np
 import pytest
@@ -284,3 +285,30 @@ def test_heads_refused():
     with pytest.raises(ValueError, match="share memory"):
         one = torch.zeros(2, 1, 4, 64).expand(2, 8, 4, 64)
         svdc.svdcache_norm_rotate(svdc.make_norm_rotate(q, None, None, one, None, None, table), q, None, None, None, None, table, one, None, None)
+
+
+# ---- angles of any base ---------------------------------------------------------------------------------------------------
+
+PI = Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899")
+
+
+def exact_turns(pos, n, theta):
+    """Angles [rows, n / 2] less whole turns, from the definition with 120 digits, and the angles themselves, as float64."""
+    with localcontext() as c:
+        c.prec = 120
+        freq = [Decimal(theta) ** (Decimal(-2 * i) / n) for i in range(n // 2)]
+        x = [[Decimal(p) * f for f in freq] for p in pos]
+        left = [[a - (a / (2 * PI)).to_integral_value() * 2 * PI for a in row] for row in x]
+    return np.array(left, dtype=np.float64), np.array(x, dtype=np.float64)
+
+
+@gpu
+@pytest.mark.parametrize("theta", [1.5, 10000.0, 5e5, 1e30, 1e300])
+def test_angles_from_exact_frequencies(theta):
+    """The bound 2^-22 + 2^-50 |x| with x from exponents that are not rounded, at any base, and at positions where the second term counts."""
+    n = 254
+    pos = [0.0, 1.0, -3.0, 12345.0, 2.0 ** 31, -(2.0 ** 40), 2.0 ** 52, 2.0 ** 60, 2.0 ** 80, -(2.0 ** 100)]
+    left, x = exact_turns(pos, n, theta)
+    got = svdc.rotary_table(torch.tensor(pos, device="cuda").unsqueeze(1), (n,), theta).cpu().double().numpy()
+    tol = 2.0 ** -22 + 2.0 ** -50 * np.abs(x)
+    assert (np.abs(got[..., 0] - np.cos(left)) <= tol).all() and (np.abs(got[..., 1] - np.sin(left)) <= tol).all()
