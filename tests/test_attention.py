@@ -507,3 +507,58 @@ def test_workspace_size_reads_what_the_call_reads(fields, spans):
     p = descriptor(**sizes, **fields)
     assert need > 0 and svdc.svdcache_attention_workspace_bytes(p) == need
     assert status(p, ws=0, **spans) == -1 and status(p, bytes=need - 1, **spans) == -6
+
+
+# ---- masks over every kernel -----------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["rows", "heads", "odd"])
+@pytest.mark.parametrize("d", [8, 64, 72, 96, 128, 200, 256, 33, 74, 130])
+@pytest.mark.parametrize("n,m", [(140, 190), (3, 2100)])
+def test_masks_at_every_width(n, m, d, layout, dtype):
+    """Left-out keys through both ways of loading, at every width that the kernels have, whole and in parts: scattered ones, whole tiles, all but the last, all."""
+    batch, h, hk = 5, 2, 1
+    g = torch.Generator().manual_seed(24)
+    q, k, v = heads(g, batch, n, h, d, dtype, layout), heads(g, batch, m, hk, d, dtype, layout), heads(g, batch, m, hk, d, dtype, layout)
+    keep = torch.zeros(batch, m, dtype=torch.bool)
+    keep[0] = torch.rand(m, generator=g) < 0.6
+    keep[1, 70:131] = True
+    keep[2, -1] = True
+    keep[4, 64:] = True
+    mask = keep.cuda()
+    for bad, of in ((float("nan"), k), (float("inf"), v), (torch.finfo(dtype).min, k)):
+        before = of[~mask].clone()
+        of[~mask] = bad
+        out = like(q)
+        call(q, k, v, out, key_mask=mask)
+        of[~mask] = before
+        for b in range(batch):
+            check(out[b], q[b], k[b][mask[b]], v[b][mask[b]], d ** -0.5, dtype)
+        assert (out[3] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["rows", "odd"])
+@pytest.mark.parametrize("d", [40, 72, 128, 136, 75])
+@pytest.mark.parametrize("most", [90, 2000])
+def test_masked_spans_at_every_width(most, d, layout, dtype):
+    """Packed sequences with masks and shared key heads through both ways of loading; rows of no span stay as they were."""
+    total = 2 * most + 50
+    g = torch.Generator().manual_seed(25)
+    q, k, v = heads(g, 1, total, 4, d, dtype, layout)[0], heads(g, 1, total, 2, d, dtype, layout)[0], heads(g, 1, total, 2, d, dtype, layout)[0]
+    q_of, k_of = [(0, 3), (3, 0), (5, 77), (90, 1), (100, 40)], [(0, most), (7, 9), (most, most), (most, 1), (2 * most, 50)]
+    mask = (torch.rand(total, generator=g) < 0.6).cuda()
+    mask[most] = False
+    k[~mask] = float("nan")
+    v[~mask] = float("inf")
+    out = torch.full((total, 4, d), 5.0, device="cuda", dtype=dtype)
+    call(q, k, v, out, *(torch.tensor(x, dtype=torch.int32, device="cuda") for x in (q_of, k_of)), mask, q_most=80, k_most=most)
+    seen = torch.zeros(total, dtype=torch.bool, device="cuda")
+    for (qa, qn), (ka, kn) in zip(q_of, k_of):
+        at = torch.arange(ka, ka + kn, device="cuda")
+        at = at[mask[at]]
+        check(out[qa:qa + qn], q[qa:qa + qn], k[at], v[at], d ** -0.5, dtype)
+        seen[qa:qa + qn] = True
+    assert (out[~seen] == 5.0).all()
