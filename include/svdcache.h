@@ -473,7 +473,8 @@ typedef struct {
  *   Qo, Ko, Vo    out  as their inputs, of dtype_out; each may be the buffer of its own input if types and strides agree.  Outputs overlap
  *                      neither each other nor inputs but so.  Rows and columns of a wider buffer that belong to no head stay.
  * At least one of Q, K, V is given.  Pointers are aligned to their elements.  Squares and their sum are float32: a head whose sum of squares passes
- * 3.4e38 gives zeros.  A head of zeros gives zeros where eps > 0. */
+ * 3.4e38 gives zeros.  mean + eps counts as 2^-126 at least: with eps = 0 a head of numbers below 2^-63 in size is multiplied by 2^63, and a head of
+ * zeros gives zeros. */
 int32_t svdcache_norm_rotate(const svdc_norm_rotate* p, const void* Q, const void* K, const void* V, const float* gain_q, const float* gain_k,
                              const float* table, void* Qo, void* Ko, void* Vo, void* stream);
 

@@ -312,3 +312,17 @@ def test_angles_from_exact_frequencies(theta):
     got = svdc.rotary_table(torch.tensor(pos, device="cuda").unsqueeze(1), (n,), theta).cpu().double().numpy()
     tol = 2.0 ** -22 + 2.0 ** -50 * np.abs(x)
     assert (np.abs(got[..., 0] - np.cos(left)) <= tol).all() and (np.abs(got[..., 1] - np.sin(left)) <= tol).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [128, 72, 33, 8, 256])
+def test_small_heads_without_eps(d, dtype):
+    """mean + eps counts as 2^-126 at least: with eps = 0 heads of numbers below 2^-63 are multiplied by 2^63, zeros stay zeros; from there on the formula holds."""
+    g = torch.Generator().manual_seed(30)
+    signs = (torch.randint(0, 2, (1, 6, 1, d), generator=g) * 2 - 1).float()
+    sizes = torch.tensor([0.0, 2.0 ** -100, 2.0 ** -70, 2.0 ** -64, 2.0 ** -62, 2.0 ** -40]).view(1, 6, 1, 1)
+    x = (signs * sizes).to(dtype).cuda()
+    got = svdc.norm_rotate(x, eps=0.0)[0].cpu().double()
+    want = torch.where(sizes < 2.0 ** -63, signs * sizes * 2.0 ** 63, signs).double()
+    assert ((got - want).abs() <= 1.01 * ((2.0 ** -8 if dtype == BF16 else 2.0 ** -24) + (d + 16) * 2.0 ** -24) * want.abs()).all()
