@@ -441,10 +441,10 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
   constexpr int PAIRS = 8 * BLOCKS;
   uint32_t over;
   float x[2][2];                                              // exponents and powers on their way
-  const auto exponents = [&](const f32x16 (&s)[BLOCKS], float by, int m) INLINE {
+  const auto exponents = [&](const f32x16 (&s)[BLOCKS], float off, float by, int m) INLINE {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      x[m % 2][e] = __builtin_fmaf(s[m / 8][2 * (m % 8) + e], a.scale, -by);
+      x[m % 2][e] = __builtin_fmaf(s[m / 8][2 * (m % 8) + e] - off, a.scale, -by);
       asm volatile("" : "+v"(x[m % 2][e]));                    // here, and not where the compiler would move it
     }
   };
@@ -469,13 +469,13 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
     }
   };
   // the n-th of `all` shares, and what is left behind the last one
-  const auto probabilities = [&](const f32x16 (&s)[BLOCKS], float by, int n, int all) INLINE {
+  const auto probabilities = [&](const f32x16 (&s)[BLOCKS], float off, float by, int n, int all) INLINE {
 #pragma unroll
     for (int m = n * PAIRS / all; m < (n + 1) * PAIRS / all; ++m) {
-      if (m == 0) exponents(s, by, 0);
+      if (m == 0) exponents(s, off, by, 0);
       if (m >= 1) operands(m - 1);
       powers(m);
-      if (m + 1 < PAIRS) exponents(s, by, m + 1);
+      if (m + 1 < PAIRS) exponents(s, off, by, m + 1);
       if (m + 1 == PAIRS) operands(m);
     }
   };
@@ -493,9 +493,11 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
   // Below 2^16 the roundings of a shift move an exponent by 2^-7 at most.  From there on (coarse) they would in the end pass SLACK, or the shift float32: the exponents are made of the
   // products' distances from the largest one, which are exact for equal products, and every tile's probabilities are made again.  (coarse is a mask in scalar registers, and the shift holds
   // that product, because the masked float32 kernel of 128 columns has no vector register left.)
-  const auto follow = [&](f32x16 (&s)[BLOCKS]) INLINE {
+  const auto follow = [&](const f32x16 (&s)[BLOCKS]) INLINE {
     constexpr uint32_t TOP = G::F32 ? 0x40000000u : 0x40004000u;
-    if ((__builtin_amdgcn_ballot_w64((over & TOP) != 0) | coarse) == 0) return;
+    // (where sums and operands do not fit the registers, what is likely decides what lies in scratch: 12 float32 heads of 256 columns, 4608 x 4608, 2.94 and 3.02 ms)
+    const bool near = (__builtin_amdgcn_ballot_w64((over & TOP) != 0) | coarse) == 0;
+    if (G::F32 && W > 128 ? __builtin_expect(near, 1) : near) return;
     float high = -INFINITY;
 #pragma unroll
     for (int t = 0; t < BLOCKS; ++t)
@@ -531,11 +533,7 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] *= less;
 #pragma unroll
-    for (int t = 0; t < BLOCKS; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[t][i] -= off;
-#pragma unroll
-    for (int n = 0; n < 8; ++n) probabilities(s, by, n, 8);
+    for (int n = 0; n < 8; ++n) probabilities(s, off, by, n, 8);
     if (!G::F32 && (over & TOP)) {                             // no number: not into a column that another query's sum comes from, but into the result
       lost = 1;
 #pragma unroll
@@ -582,7 +580,7 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
       const auto keys_tile = tile_of(K, a.k.row, k_row, tile + 2), values_tile = tile_of(V, a.v.row, v_row, tile + 1);
       if (!DIRECT) take_keys(tile + 2, keep[2]);
       multiply_keys(s_next, keys_next, [&](int n, int all) INLINE {
-        probabilities(s, shift, n, all);
+        probabilities(s, 0.f, shift, n, all);
 #pragma unroll
         for (int j = n * 2 * LOADS / all; DIRECT && j < (n + 1) * 2 * LOADS / all; ++j) {
           if (j < LOADS)
@@ -612,7 +610,7 @@ __device__ __forceinline__ void attend(const AttentionArgs& a) {
     }
     begin();
 #pragma unroll
-    for (int n = 0; n < 8; ++n) probabilities(s0, shift, n, 8);
+    for (int n = 0; n < 8; ++n) probabilities(s0, 0.f, shift, n, 8);
     follow(s0);
     first_values(columns0.b);
     multiply_values(columns0.b);
