@@ -492,8 +492,9 @@ typedef struct {
   svdc_heads q, k, v, o;         /* seq is not read where spans are given */
 } svdc_attention;
 
-/* Bytes of device workspace that svdcache_attention needs: 0 where the rows of queries fill the card (and for an invalid one); few rows over
- * many keys keep the results of parts of the keys there.  Spans and masks do not change it. */
+/* Bytes of device workspace that svdcache_attention needs, for the results of parts of the keys: where few rows of queries have many keys, and where the
+ * tiles of queries fill the last round of compute units in part only (4608 x 4608 with 24 heads of 128: 13 MB).  Else, and for an invalid one, 0.
+ * Spans and masks do not change it. */
 size_t svdcache_attention_workspace_bytes(const svdc_attention* p);
 
 /* Out = softmax(scale * Q K^T) V for each sequence and head; every query sees all keys of its sequence that the mask leaves.
@@ -510,7 +511,8 @@ size_t svdcache_attention_workspace_bytes(const svdc_attention* p);
  *                  call until it has completed on the stream: calls in flight on different streams need one each.
  * Pointers are aligned to their elements; rows and heads at multiples of 16 bytes of one another (pointers, strides and head_dim) are read faster.
  * Products and sums, the softmax's maximum and sum are float32.  Products that float32 holds give finite results, however large scale times them is.  For bfloat16 the probabilities enter the second product rounded to
- * bfloat16, which is as much off as rounding the result is; float32 uses float32 products throughout.  The exponential is the hardware's power of two (a step of the last place).  Results do not depend on anything but the
+ * bfloat16, and so does their sum: a result is off by at most 2^-8 sum p |v| for it, which is more than rounding it where values cancel, and a few
+ * hundredths of that on random ones; float32 uses float32 products throughout.  The exponential is the hardware's power of two (a step of the last place).  Results do not depend on anything but the
  * arguments and the number of compute units (no atomics). */
 int32_t svdcache_attention(const svdc_attention* p, const void* Q, const void* K, const void* V, const int32_t* q_span, const int32_t* k_span,
                            const uint8_t* key_mask, void* Out, void* workspace, size_t workspace_bytes, void* stream);

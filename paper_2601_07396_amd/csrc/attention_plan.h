@@ -42,11 +42,15 @@ inline AttentionPlan attention_plan(const svdc_attention& p, int cus) {
   const int rest = plan.units % cus;
   if (plan.units > 0 && plan.units < cus) {
     // Fewer units than compute units: parts of all, until each of these has two workgroups.  64 x 119056, 24 heads: 21 parts 270 us.  1 x 512, 24 heads: 4 parts 8.7 us,
-    // whole 10.5
+    // whole 10.5.  One to three units stay below that, as the join has a lane for each part: 1 x 119056, one head of keys, 63 workgroups 43 us, 1.4 TB/s; three heads 51 us, 3.6 TB/s.
     cut(0, std::min<int64_t>(std::min<int64_t>(std::max(1, 2 * cus / plan.units), kMostParts), (tiles + kLeastTiles - 1) / kLeastTiles));
   } else if (rest) {
     // The last round has work for some of the compute units only: its units in parts, if that takes less than what the parts' sums cost on their way through memory.
-    // 4608 x 4608, 24 heads, 864 units: the last 96 in 5 parts 246 us, whole 259; 4 sequences of it 949 and 965; 29764 x 29764, 3 heads 1.20 and 1.25 ms
+    // 4608 x 4608, 24 heads, 864 units: the last 96 in 2 parts 234 us, whole 250; 4 sequences of it 911 and 919; 29764 x 29764, 3 heads, 4 parts 1.15 ms, whole 1.21; float32, 24 heads,
+    // 8 parts 1.83, whole 2.16 ms
+    // The constants are us, read off such calls of 128 columns: a round of 4608 keys takes 62 us in bfloat16 and 530 in float32, a part's sums are written and read at 4 TB/s, a launch
+    // takes 5.  Narrower heads take longer than their share of a round says (4608 keys of 64 columns 43 us, not 31), but there, too, the 2 parts that this gives were the fastest of 1 to 8
+    // (64 columns 144 us, whole 154; 72 columns 186 and 200).
     const double round = tiles * keys * (width / 128.0) * (p.dtype == SVDC_F32 ? 0.115 : 0.0135), sums = 2.0 * kTileQueries * width * 4 / 4e6;
     double least = round;
     int64_t best = 1;

@@ -4,7 +4,8 @@
 // Both stream their rows once and reuse next to nothing.  Norm and rotation are bound by memory (a copy of 1 GiB reaches 5.2 TB/s):
 //     4608 rows, 24 + 24 heads of 128, bfloat16 (116 MB) 25.7 us, 4.5 TB/s, 21.9 of it in the kernel; 4 x 4096 rows, float32 into bfloat16 with values (908 MB) 172 us, 5.3 TB/s
 //     odd heads: 3 x 1001 rows, 16 + 8 heads of 72, 27 pairs of halves, float32 (42 MB) 12.7 us; one row 4.1 us, a launch
-// The angles are bound by their arithmetic in 64 bits: 119056 x 64 pairs (62 MB) 16 us, 3.9 TB/s; 4608 x 64 4.1 us.
+// The angles: 119056 x 64 pairs (62 MB) 16-17 us, 3.8 TB/s; 4608 x 64 4.1 us.  Of 17.2 us the stores alone, 8 bytes a lane, take 13.7 (4.5 TB/s), the powers in 64 bits that every
+// workgroup begins with 2.7, and reduction and series beside the stores 1.4 (each left out in turn).
 #include <algorithm>
 #include <cmath>
 
