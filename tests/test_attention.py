@@ -466,6 +466,27 @@ def test_large_logits_beside_ordinary_ones(n, m, dtype):
         assert torch.isfinite(out[0, 5]).all() if math.isfinite(bad) else out[0, 5].isnan().all()
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("steps,scale", [((20, 14), 2.0 ** -3), ((60, 50), 2.0 ** 20)])
+@pytest.mark.parametrize("n,m,d", [(150, 300, 128), (3, 3000, 128), (40, 700, 74)])
+def test_large_logits_under_a_mask(n, m, d, steps, scale, dtype):
+    """The largest logits left out, whole tiles and parts without keys among the others, one key, none; heads that share keys."""
+    q, k, v = whole_numbers(n, m, d, dtype, seed=26)
+    q, k, v = (q * 2.0 ** steps[0]).expand(4, -1, -1, -1), (k * 2.0 ** steps[1])[:, :, :1].repeat(4, 1, 1, 1), v[:, :, :1].repeat(4, 1, 1, 1)
+    keep = torch.zeros(4, m, dtype=torch.bool)
+    keep[0] = torch.rand(m, generator=torch.Generator().manual_seed(27)) < 0.5
+    keep[1, 130:250] = True
+    keep[2, -2] = True
+    keep = keep.cuda()
+    k[~keep], v[~keep] = torch.finfo(dtype).max, float("nan")
+    out = torch.full(q.shape, float("nan"), device="cuda", dtype=dtype)
+    call(q, k, v, out, key_mask=keep, scale=scale)
+    for b in range(3):
+        check_exact_products(out[b], q[b], k[b][keep[b]], v[b][keep[b]], scale, dtype)
+    assert (out[3] == 0).all()
+
+
 # ---- what lies in the tensors reaches the result, whole and in parts ---------------------------------------------------
 
 @gpu
